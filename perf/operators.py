@@ -331,8 +331,8 @@ def run(st):
         F.token_logprobs(x, ld, T, S, B, V, st["tok"], st["par"], k, o["logp"], o["entropy"], o["lse"], tops, vals)
         if kind == "score":
             return (o["logp"], o["entropy"], o["lse"]) + st["top"]
-        F.token_logprobs_backward(x, ld, T, S, B, V, st["tok"], st["par"], o["lse"], o["entropy"], st["gl"], st["ge"],
-                                  st["grad"], V)
+        F.token_logprobs_backward(x, ld, T, S, B, V, st["tok"], st["par"], o["logp"], o["entropy"], o["lse"], st["gl"],
+                                  st["ge"], st["grad"], V)
         return o["logp"], o["entropy"], o["lse"], st["grad"]
     if kind == "joint":
         o = st["out"]
