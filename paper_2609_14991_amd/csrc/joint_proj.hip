@@ -5,211 +5,33 @@
 //   out[m, n] = sum_k A[m, k] * W[n, k] + bias[n]      (bf16 inputs, fp32 accumulate)
 //
 // A is [M, K] and W is [N, K], both row-major bf16 (W in the usual layout of a
-// linear layer's weight), so both MFMA operands are contiguous along K.
-//
-// Tiling for gfx950: a workgroup of WM x WN waves computes a (16 TM WM) x
-// (16 TN WN) output tile, each wave (16 TM) x (16 TN) as a TM x TN grid of
-// v_mfma_f32_16x16x32_bf16 tiles.  K advances in stages of 64, NB of them in
-// LDS; the operands go straight from global memory to LDS (16 bytes a lane, no
-// registers, no LDS store instructions), NB - 1 stages ahead, with one barrier
-// a stage that waits for the oldest stage's loads only.  A stage's rows are 128
-// bytes, all LDS banks, so a fragment read (16 rows, one 16-byte chunk of each)
-// would hit the same banks in every row: chunk c of row r is kept in slot
-// c ^ (r % 8), which the loading lane arranges by the global chunk it picks.
-// SQ_LDS_BANK_CONFLICT reads 0 (rows padded by 16 bytes: 47 % of the LDS's
-// active cycles).  The MFMA operands are swapped (W rows as the tile's rows),
-// so a lane ends with 4 consecutive columns of one output row.
+// linear layer's weight), so both MFMA operands are contiguous along K.  The
+// tiles are joint_tile.h's.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "fusion_internal.h"
+#include "joint_tile.h"
 
 namespace fusion {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kBK = 64;                       // K per stage
-constexpr int kMapNone = 0, kMap4x2 = 1, kMapRuns = 2;  // tiles to XCDs
-constexpr uint32_t kOutside = 0x80000000u;    // an offset past every descriptor (operands are under 2 GiB)
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void *base, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), (short)0, (int)bytes, 0x00020000);
-}
-// 16 bytes per lane straight into LDS (lane l lands at lds + 16 l)
-__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, unsigned char *lds, uint32_t voff, uint32_t soff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)lds, 16, voff, soff, 0, 0);
-}
-// Barrier that also waits for this wave's LDS reads and for all but its N newest
-// vector-memory operations (the loads into LDS count there, in order)
-template <int N>
-__device__ __forceinline__ void wait_barrier() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
-
-// kWM x kWN waves, each a (16 kTM) x (16 kTN) output tile; kNB stages in LDS;
-// kAux: cache policy of the output stores (see joint_project)
-template <int kWM, int kWN, int kTM, int kTN, int kNB, int kAux>
-__global__ void __launch_bounds__(64 * kWM * kWN, 2) joint_proj_kernel(const uint16_t *__restrict__ A,
-                                                                        const uint16_t *__restrict__ W,
-                                                                        const float *__restrict__ bias, int M, int N,
-                                                                        int K, int n_col_tiles, int map,
-                                                                        float *__restrict__ out) {
-  constexpr int kRM = 16 * kTM, kRN = 16 * kTN;  // rows and columns of a wave's tile
-  constexpr int kBM = kRM * kWM, kBN = kRN * kWN, kWaves = kWM * kWN;
-  constexpr int kChunks = kBK / 8;               // 16-byte chunks per row and stage
-  constexpr int kRowsPer = 64 / kChunks;         // rows one wave-wide load brings (1 KiB)
-  constexpr int kLA = kBM / kRowsPer / kWaves, kLW = kBN / kRowsPer / kWaves, kL = kLA + kLW;  // loads per wave
-  static_assert(kLA * kRowsPer * kWaves == kBM && kLW * kRowsPer * kWaves == kBN, "whole loads per wave");
-  constexpr int kStage = (kBM + kBN) * kBK * 2;  // bytes of a stage
-  constexpr int kSeg = kRN < 64 ? kRN : 64, kLanes = kSeg / 4, kRowsI = 64 / kLanes;  // epilogue: see there
-  static_assert(kNB * kStage >= kWaves * 16 * kSeg * 4, "LDS too small for the epilogue");
-  __shared__ __align__(1024) unsigned char smem[kNB * kStage];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // tile of this workgroup, which runs on XCD x = blockIdx % 8 under the hardware's
-  // round-robin (see joint_project for the choice):
-  // kMap4x2 (row tiles a multiple of 4, column tiles even): XCD x takes the row
-  // tiles = x % 4 (mod 4) against column half x / 4, so a row band of A is fetched by
-  // two XCDs instead of eight and each XCD's L2 keeps half of W.
-  // kMapRuns: each XCD takes a run of consecutive tiles, column-fastest, so that a row
-  // band of A is fetched by one XCD (two at a run's end) and every L2 holds W.
-  // kMapNone: column-fastest over all XCDs
+template <class S, int kAux>
+__global__ void __launch_bounds__(64 * S::waves, 2) joint_proj_kernel(const uint16_t *__restrict__ A,
+                                                                     const uint16_t *__restrict__ W,
+                                                                     const float *__restrict__ bias, int M, int N,
+                                                                     int K, int n_col_tiles, int map,
+                                                                     float *__restrict__ out) {
+  __shared__ __align__(1024) unsigned char smem[S::lds];
   int tr, tc;
-  if (map == kMap4x2) {
-    const int x = blockIdx.x & 7, i = blockIdx.x >> 3;
-    const int half = n_col_tiles >> 1;
-    tr = (i / half) * 4 + (x & 3);
-    tc = (x >> 2) * half + i % half;
-  } else {
-    int t = blockIdx.x;
-    if (map == kMapRuns) {
-      const int x = t & 7, per = gridDim.x >> 3, more = gridDim.x & 7;  // the first `more` XCDs take one tile more
-      t = x * per + min(x, more) + (t >> 3);
-    }
-    tr = t / n_col_tiles;
-    tc = t % n_col_tiles;
-  }
-  const int bn = tc * kBN, bm = tr * kBM;
-  const int wm = (wave / kWN) * kRM, wn = (wave % kWN) * kRN;
-
-  // Load j of a stage brings rows (j * kWaves + wave) * kRowsPer .. of A (j < kLA)
-  // or W to consecutive LDS: lane l lands 16 l bytes in, i.e. row l / 8, slot
-  // l % 8, and fetches the chunk which that slot holds.  Rows past the operand
-  // and, in a ragged last stage, chunks past K read as zeros (range check).
-  const __amdgpu_buffer_rsrc_t ra = rsrc(A, (uint32_t)((int64_t)M * K * 2));
-  const __amdgpu_buffer_rsrc_t rw = rsrc(W, (uint32_t)((int64_t)N * K * 2));
-  const int lr = lane / kChunks, lc = (lane % kChunks) ^ (lr & 7);  // kRowsPer is 8: the row's low bits are lr
-  uint32_t vo[kL];
-#pragma unroll
-  for (int j = 0; j < kL; ++j) {
-    const int row = (j < kLA ? bm + (j * kWaves + wave) * kRowsPer : bn + ((j - kLA) * kWaves + wave) * kRowsPer) + lr;
-    vo[j] = row < (j < kLA ? M : N) ? (uint32_t)(((int64_t)row * K + lc * 8) * 2) : kOutside;
-  }
-  auto issue = [&](int s, int buf) {
-    unsigned char *base = smem + buf * kStage + wave * 1024;
-    const bool ragged = (s + 1) * kBK > K && s * kBK + lc * 8 >= K;
-#pragma unroll
-    for (int j = 0; j < kL; ++j)
-      load_lds(j < kLA ? ra : rw, base + j * kWaves * 1024, ragged ? kOutside : vo[j], s * kBK * 2);
-  };
-
-  f32x4 acc[kTM][kTN];
-#pragma unroll
-  for (int i = 0; i < kTM; ++i)
-#pragma unroll
-    for (int j = 0; j < kTN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  const int nk = (K + kBK - 1) / kBK;
-#pragma unroll
-  for (int s = 0; s < kNB - 1; ++s)
-    if (s < nk) issue(s, s);
-  // fragment of a 16 x 32 operand tile: lane l holds row l % 16, K elements 8 * (l / 16) .. + 7
-  const int fr = lane & 15, fc = lane >> 4;
-  int buf = 0;
-  for (int s = 0; s < nk; ++s) {
-    // stage s has landed for every wave, and every wave is done reading the
-    // buffer of stage s - 1, which stage s + kNB - 1 is loaded into
-    if (s + kNB - 2 < nk) wait_barrier<(kNB - 2) * kL>();
-    else wait_barrier<0>();
-    if (s + kNB - 1 < nk) issue(s + kNB - 1, buf == 0 ? kNB - 1 : buf - 1);
-    const unsigned char *pa = smem + buf * kStage, *pw = pa + kBM * kBK * 2;
-#pragma unroll
-    for (int ks = 0; ks < kBK / 32; ++ks) {
-      bf16x8 fa[kTM], fw[kTN];
-#pragma unroll
-      for (int j = 0; j < kTN; ++j)
-        fw[j] = *reinterpret_cast<const bf16x8 *>(pw + (wn + j * 16 + fr) * kBK * 2 + (((ks * 4 + fc) ^ (fr & 7)) * 16));
-#pragma unroll
-      for (int i = 0; i < kTM; ++i)
-        fa[i] = *reinterpret_cast<const bf16x8 *>(pa + (wm + i * 16 + fr) * kBK * 2 + (((ks * 4 + fc) ^ (fr & 7)) * 16));
-#pragma unroll
-      for (int i = 0; i < kTM; ++i)
-#pragma unroll
-        for (int j = 0; j < kTN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[j], fa[i], acc[i][j], 0, 0, 0);
-    }
-    buf = buf == kNB - 1 ? 0 : buf + 1;
-  }
-
-  // Epilogue.  In the accumulator of a 16 x 16 tile lane l holds output row l %
-  // 16, columns 4 * (l / 16) .. + 3.  Each 16-row slab of the wave's tile goes
-  // through the wave's own LDS area (free once every wave has read the last
-  // stage), chunks swizzled by the row as above, and leaves as whole row segments
-  // of kSeg columns, kRowsI rows a store.  The bias is fetched before the first
-  // store: a load behind stores would wait for all of them.
-  float bv[kRN / kSeg][4];
-#pragma unroll
-  for (int sg = 0; sg < kRN / kSeg; ++sg)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = bn + wn + sg * kSeg + (lane % kLanes) * 4 + r;
-      bv[sg][r] = (bias && n < N) ? bias[n] : 0.0f;
-    }
-  wait_barrier<0>();
-  f32x4 *slab = reinterpret_cast<f32x4 *>(smem) + wave * 16 * kLanes;
-  const int orow = lane / kLanes, ochunk = lane % kLanes;
-#pragma unroll
-  for (int i = 0; i < kTM; ++i) {
-#pragma unroll
-    for (int sg = 0; sg < kRN / kSeg; ++sg) {
-#pragma unroll
-      for (int j = 0; j < kSeg / 16; ++j)
-        slab[fr * kLanes + ((j * 4 + fc) ^ (fr & (kLanes - 1)))] = acc[i][sg * (kSeg / 16) + j];
-      __builtin_amdgcn_wave_barrier();
-      const int n = bn + wn + sg * kSeg + ochunk * 4;
-#pragma unroll
-      for (int q = 0; q < 16 / kRowsI; ++q) {
-        const int row = q * kRowsI + orow;
-        const f32x4 x = slab[row * kLanes + (ochunk ^ (row & (kLanes - 1)))];
-        i32x4 v;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = __float_as_int(x[r] + bv[sg][r]);
-        // a descriptor of this store's rows that exist; columns past N fall outside it
-        const int m0 = bm + wm + i * 16 + q * kRowsI;
-        const int rows = min(max(M - m0, 0), kRowsI);
-        const __amdgpu_buffer_rsrc_t ro = rsrc(out + (int64_t)m0 * N, (uint32_t)rows * (uint32_t)N * 4u);
-        const uint32_t o = ((uint32_t)orow * (uint32_t)N + (uint32_t)n) * 4u;
-        __builtin_amdgcn_raw_buffer_store_b128(v, ro, n + 3 < N ? o : kOutside, 0, kAux);
-        if (N % 4 != 0) {  // uniform: the row's last columns, one at a time
-#pragma unroll
-          for (int r = 0; r < 3; ++r)
-            __builtin_amdgcn_raw_buffer_store_b32(v[r], ro, (n + 3 >= N && n + r < N) ? o + 4 * r : kOutside, 0, kAux);
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
-    }
-  }
+  tile_place(map, n_col_tiles, tr, tc);
+  f32x4 acc[S::TM][S::TN];
+  Bf16Op op;
+  tile_product<S>(op, smem, A, W, M, N, K * 2, tr * S::BM, tc * S::BN, acc);
+  tile_store<S, kAux>(smem, bias, M, N, tr * S::BM, tc * S::BN, acc, out);
 }
-
-// a launch shape of joint_proj_kernel
-template <int WM_, int WN_, int TM_, int TN_, int NB_>
-struct ProjCfg {
-  static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NB = NB_;
-  static constexpr int BM = 16 * TM_ * WM_, BN = 16 * TN_ * WN_;
-};
 
 }  // namespace
 }  // namespace fusion
@@ -225,12 +47,12 @@ extern "C" int joint_project(const uint16_t *A, const uint16_t *W, const float *
   if (M == 0) return FUSION_OK;
   if (!A || !W || !out) return set_error(FUSION_E_ARG, "NULL operand");
   if (((uintptr_t)A | (uintptr_t)W) % 16 != 0) return set_error(FUSION_E_ARG, "A and W must be 16-byte aligned");
-  constexpr ProjCfg<2, 4, 8, 4, 2> t256{};
-  constexpr ProjCfg<2, 2, 4, 4, 2> t128{};
-  constexpr ProjCfg<2, 2, 2, 4, 2> t64x128_3a_cu{};
-  constexpr ProjCfg<2, 2, 2, 4, 3> t64x128{};
-  constexpr ProjCfg<2, 2, 2, 2, 4> t64{};
-  constexpr ProjCfg<2, 2, 1, 2, 4> t32{};
+  constexpr TileShape<2, 4, 8, 4, 2> t256{};
+  constexpr TileShape<2, 2, 4, 4, 2> t128{};
+  constexpr TileShape<2, 2, 2, 4, 2> t64x128_3a_cu{};
+  constexpr TileShape<2, 2, 2, 4, 3> t64x128{};
+  constexpr TileShape<2, 2, 2, 2, 4> t64{};
+  constexpr TileShape<2, 2, 1, 2, 4> t32{};
   constexpr int64_t kCus = 256;
   auto tiles = [&](auto cfg) -> int64_t {
     using C = decltype(cfg);
@@ -240,25 +62,17 @@ extern "C" int joint_project(const uint16_t *A, const uint16_t *W, const float *
     using C = decltype(cfg);
     const int nct = (N + C::BN - 1) / C::BN, nrt = (M + C::BM - 1) / C::BM;
     if (tiles(cfg) > 0x7FFFFFFFll) return set_error(FUSION_E_UNSUPPORTED, "too many tiles");
-    // Tiles to XCDs: 4 x 2 where the tiles divide so; else, in a launch of more than a
-    // round, in runs if W fits an L2 (up to 4 MB), has at most 32 column tiles and is
-    // the smaller operand.  Not dealt at all, 128 x 128 tiles fetch every row band of A on
-    // all eight XCDs: 30343 x 1024 x 248 45 us, in runs 36; 48340 x 1024 x 768 117 and 88;
-    // over 190 random sizes that the rule takes 5 % (M < 2 N) to 14 % (M > 8 N) faster in
-    // runs, 256 x 256 tiles 4 to 5 %.  Against 4 x 2 runs gain 7 % to lose 19 %.
-    const bool by4x2 = nrt % 4 == 0 && nct % 2 == 0;
-    const bool runs = tiles(t128) > kCus && M >= N && nct <= 32 && (int64_t)N * K * 2 <= 4 << 20;
-    const int map = by4x2 ? kMap4x2 : runs ? kMapRuns : kMapNone;
+    const int map = tile_map(nrt, nct, tiles(t128) > kCus, M, N, (int64_t)N * K * 2);
     // Rows of whole 128-byte lines leave as streaming stores (nt with sc1: 459 us
     // for 76800 x 4096 x 640, plain 535, launches back to back); rows that share lines with their
     // neighbours are left for the L2 to merge (76800 x 1001 x 136: 91 us plain,
     // over 100 streaming)
-    const dim3 grid(nct * nrt), block(64 * C::WM * C::WN);
+    const dim3 grid(nct * nrt), block(64 * C::waves);
     if (N % 32 == 0)
-      hipLaunchKernelGGL((joint_proj_kernel<C::WM, C::WN, C::TM, C::TN, C::NB, 18>), grid, block, 0, stream, A, W, bias,
+      hipLaunchKernelGGL((joint_proj_kernel<C, 18>), grid, block, 0, stream, A, W, bias,
                          M, N, K, nct, map, out);
     else
-      hipLaunchKernelGGL((joint_proj_kernel<C::WM, C::WN, C::TM, C::TN, C::NB, 0>), grid, block, 0, stream, A, W, bias,
+      hipLaunchKernelGGL((joint_proj_kernel<C, 0>), grid, block, 0, stream, A, W, bias,
                          M, N, K, nct, map, out);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? FUSION_OK : hip_error(e, "joint projection launch");
