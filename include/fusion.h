@@ -74,7 +74,11 @@ enum {
 
 /* status bits reported by fusion_device_status */
 enum { FUSION_STATUS_BAD_LM_STATE = 1, FUSION_STATUS_BAD_BOOST_STATE = 2,
-       FUSION_STATUS_SYNC_TIMEOUT = 4 /* a beam stream's workgroups failed to meet (results invalid) */ };
+       FUSION_STATUS_SYNC_TIMEOUT = 4, /* a beam stream's workgroups failed to meet (results invalid) */
+       FUSION_STATUS_BAD_TOKEN = 8     /* a token or parent to score is out of range */ };
+
+/* element types of logits to score and of rows to quantise */
+enum { FUSION_F32 = 0, FUSION_BF16 = 1, FUSION_F16 = 2 };
 
 /* limits of this build */
 #define FUSION_MAX_ORDER 6   /* n-gram order N (the per-level registers of the fusion kernel are sized for it) */
@@ -82,6 +86,7 @@ enum { FUSION_STATUS_BAD_LM_STATE = 1, FUSION_STATUS_BAD_BOOST_STATE = 2,
 #define FUSION_MAX_K 8
 #define FUSION_MAX_BEAM 32
 #define FUSION_MAX_LMS 2     /* LMs per fusion_step_lms / fusion_run_lms call (2 needs V <= 4096) */
+#define FUSION_MAX_SCORED_VOCAB (1 << 24) /* token_logprobs */
 
 /* flags of fusion_run_lms */
 #define FUSION_RUN_RECOMBINE 1 /* beam: merge candidates that reach the same history */
@@ -340,6 +345,114 @@ int fusion_run_projected(const NgramTables *const *lms, const float *alphas, int
                          int32_t chunk, int32_t T, int32_t S, int32_t B, int32_t V, int32_t k, float beta, int32_t blank_id,
                          int32_t blank_mode, int32_t *lm_state, int32_t *boost_state, double *hyp_score,
                          int32_t *tokens, int32_t *parents, int32_t flags, uint64_t *hist, hipStream_t stream);
+
+/*
+ * token_logprobs - how sure the acoustic distribution was of the tokens a decode
+ * chose (Eq. (1)'s log p_AM(y|x) of each, without LM and boost terms): per token
+ * its log probability, the entropy of the distribution it was chosen from and the
+ * best alternatives.
+ *   logits       device [T, H, V], H = S * B, of type dtype (FUSION_F32, FUSION_BF16
+ *                or FUSION_F16), rows `stride` elements apart (stride >= V), aligned
+ *                to its elements
+ *   V            1..FUSION_MAX_SCORED_VOCAB; T * H < 2^24
+ *   tokens       device [T, H], as fusion_run leaves them: -1 for none.  NULL where
+ *                logp is NULL
+ *   parents      device [T, H] or NULL, as fusion_run leaves them: the token of slot b
+ *                of stream s at frame t was chosen on row (t, s * B + parents[t, s * B + b]);
+ *                -1 for a dead slot.  Needs B <= FUSION_MAX_BEAM.  NULL: on row (t, s * B + b)
+ *   k            0..FUSION_MAX_K alternatives
+ *   logp         [T, H] fp32 or NULL: x[token] - lse(x); 0 without a token or row
+ *   entropy      [T, H] fp32 or NULL: -sum p log p in nats; 0 without a row
+ *   lse          [T, H] fp32 or NULL: log sum exp of the row; -inf without a row
+ *   top_tokens, top_logp  [T, H, k]: the k largest logits of the row, best first, ties to
+ *                the lowest id, and their log probabilities; -1 and -inf where a row has
+ *                fewer that are not -inf, and without a row
+ * At least one output is asked for.  Arithmetic is fp32 whatever dtype is.  Logits
+ * of -inf (and of the type's lowest value) are masked tokens.  A row of -inf alone
+ * has lse and every log probability -inf, entropy 0 and no alternatives; a row with
+ * a NaN or +inf has NaN for all three, and alternatives -1 with NaN.  A token
+ * outside [-1, V) gets logp NaN, a parent outside [-1, B) NaN in every output, and
+ * FUSION_STATUS_BAD_TOKEN is set.  Only enqueues work on `stream`; no workspace.
+ */
+int token_logprobs(const void *logits, int32_t dtype, int64_t stride, int32_t T, int32_t S, int32_t B, int32_t V,
+                   const int32_t *tokens, const int32_t *parents, int32_t k, float *logp, float *entropy, float *lse,
+                   int32_t *top_tokens, float *top_logp, hipStream_t stream);
+
+/*
+ * token_logprobs_backward - the gradient of token_logprobs with respect to the logits,
+ *   grad[row, y] = sum over the tokens chosen on the row of
+ *                  grad_logp * (1[y = token] - p_y) - grad_entropy * p_y * (log p_y + entropy)
+ *   logits .. parents  as in token_logprobs
+ *   logp, entropy, lse  device [T, H]: what token_logprobs gave for the same inputs
+ *                (logp may be NULL without grad_logp, entropy without grad_entropy)
+ *   grad_logp, grad_entropy  device [T, H] fp32 incoming gradients; either may be NULL, not both.
+ *                A slot without a row contributes nothing, one without a token only
+ *                its entropy's gradient
+ *   grad_logits  device [T, H, V] of type dtype, rows `grad_stride` elements apart,
+ *                written whole: 0 for a row on which no token was chosen and for one of
+ *                -inf alone, NaN for one with a NaN or +inf.  May be logits itself with
+ *                the same stride; otherwise the two must not overlap
+ * Sums are fp32 in a fixed order, rounded once to dtype.  The alternatives have no
+ * gradient.  Tokens and parents out of range contribute nothing and set
+ * FUSION_STATUS_BAD_TOKEN.  Only enqueues work on `stream`; no workspace.
+ */
+int token_logprobs_backward(const void *logits, int32_t dtype, int64_t stride, int32_t T, int32_t S, int32_t B,
+                            int32_t V, const int32_t *tokens, const int32_t *parents, const float *logp,
+                            const float *entropy, const float *lse, const float *grad_logp, const float *grad_entropy,
+                            void *grad_logits, int64_t grad_stride, hipStream_t stream);
+
+/*
+ * joint_logprobs - token_logprobs straight from the joint's hidden states, for
+ * callers that do not keep the logits (fusion_run_projected leaves the last chunk's
+ * only): the statistics of joint_project's output rows, which are never stored.
+ *   A, W, bias, K  as in joint_project, A [T, S * B, K], W [V, K]
+ *   tokens, parents, logp, entropy, lse  as in token_logprobs (no alternatives: for
+ *                those project a chunk and call token_logprobs)
+ *   workspace    device, workspace_floats >= what joint_logprobs_workspace(T * S * B, V, K)
+ *                gives; its contents before and after mean nothing.  Calls that may
+ *                overlap, graphs among them, need one each
+ * Logits are joint_project's up to the order of a fp32 sum.  Forward only: train
+ * with joint_project, token_logprobs and token_logprobs_backward.  Sizes and
+ * alignment as for joint_project; only enqueues work on `stream`.
+ */
+int joint_logprobs_workspace(int32_t M, int32_t V, int32_t K, int64_t *floats);
+int joint_logprobs(const uint16_t *A, const uint16_t *W, const float *bias, int32_t K, int32_t T, int32_t S, int32_t B,
+                   int32_t V, const int32_t *tokens, const int32_t *parents, float *logp, float *entropy, float *lse,
+                   float *workspace, int64_t workspace_floats, hipStream_t stream);
+
+/*
+ * mx_quantize / mx_dequantize - rows in microscaled 4-bit floating point and back.
+ * A block of 32 consecutive values of a row shares a power of two 2^e, the byte e + 127;
+ * a value is 4 bits, sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0..7, sign bit 8),
+ * two to a byte, the value of even index in the low half.
+ *   e = max(floor(log2(largest magnitude of the block)) - 2, -127); x / 2^e is rounded to
+ *   the nearest level, halfway to the even code, beyond 6 to 6.  A block with a NaN or an
+ *   infinity has scale byte 255 and elements 0, and is NaN read back.
+ *   x            device [R, K] of type dtype, rows `stride` >= K elements apart, aligned to its elements
+ *   K            a multiple of 32 (FUSION_E_UNSUPPORTED otherwise); R >= 0 (0 does nothing)
+ *   q            device [R, K / 2], 16-byte aligned
+ *   scales       device [R, FUSION_MX_SCALE_STRIDE(K)], 8-byte aligned: a row's K / 32 scale
+ *                bytes, then zeros to a multiple of 8 (written by mx_quantize, not read by the others)
+ *   out          device [R, K] of type dtype, rows `stride` >= K apart: element * 2^e, rounded once
+ */
+#define FUSION_MX_SCALE_STRIDE(K) (((K) / 32 + 7) / 8 * 8)
+int mx_quantize(const void *x, int32_t dtype, int64_t stride, int32_t R, int32_t K, uint8_t *q, uint8_t *scales,
+                hipStream_t stream);
+int mx_dequantize(const uint8_t *q, const uint8_t *scales, int32_t R, int32_t K, void *out, int32_t dtype,
+                  int64_t stride, hipStream_t stream);
+
+/*
+ * joint_project_mx - joint_project with both operands in the format of mx_quantize:
+ *     out[m, n] = sum over blocks of 2^(eA + eW) * sum_32 a * w, + bias[n]
+ *   A, A_scales  device [M, K / 2], [M, FUSION_MX_SCALE_STRIDE(K)]: quantised hidden states
+ *   W, W_scales  device [N, K / 2], [N, FUSION_MX_SCALE_STRIDE(K)]: the quantised weight
+ *   bias, out    as in joint_project
+ * Products are exact, sums fp32 in an unspecified order.  A row with a NaN block is
+ * NaN.  K a multiple of 32, each operand under 2 GiB, N < 2^25 (FUSION_E_UNSUPPORTED
+ * otherwise); A and W 16-byte aligned, scales 8-byte.  Only enqueues work on `stream`.
+ */
+int joint_project_mx(const uint8_t *A, const uint8_t *A_scales, const uint8_t *W, const uint8_t *W_scales,
+                     const float *bias, int32_t M, int32_t N, int32_t K, float *out, hipStream_t stream);
 
 /* description of the calling thread's last failure (library-owned string) */
 const char *fusion_last_error(void);

@@ -32,6 +32,9 @@ FUSION_BLANK_AM = 0
 FUSION_BLANK_COMPETE = 1
 FUSION_STATUS_BAD_LM_STATE = 1
 FUSION_STATUS_BAD_BOOST_STATE = 2
+FUSION_STATUS_BAD_TOKEN = 8
+
+FUSION_F32, FUSION_BF16, FUSION_F16 = 0, 1, 2
 
 FUSION_MAX_LMS = 2
 FUSION_RUN_RECOMBINE = 1
@@ -39,7 +42,9 @@ FUSION_RUN_RECOMBINE = 1
 EXPORTS = ("ngram_load", "ngram_bos_state", "ngram_info", "ngram_free", "boost_build", "boost_info",
            "boost_free", "fusion_step", "fusion_run", "fusion_step_lms", "fusion_run_lms",
            "fusion_run_lms_noalloc", "fusion_run_projected",
-           "fusion_end_scores", "joint_project", "fusion_last_error", "fusion_device_status")
+           "fusion_end_scores", "joint_project", "token_logprobs", "token_logprobs_backward",
+           "joint_logprobs_workspace", "joint_logprobs", "mx_quantize", "mx_dequantize", "joint_project_mx",
+           "fusion_last_error", "fusion_device_status")
 
 
 class FusionError(RuntimeError):
@@ -96,6 +101,20 @@ def lib():
         L.fusion_end_scores.argtypes = [vp, vp, i32, vp, i32, vp, vp, vp]
         L.joint_project.restype = ctypes.c_int
         L.joint_project.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
+        L.token_logprobs.restype = ctypes.c_int
+        L.token_logprobs.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+        L.token_logprobs_backward.restype = ctypes.c_int
+        L.token_logprobs_backward.argtypes = [vp, i32, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.joint_logprobs_workspace.restype = ctypes.c_int
+        L.joint_logprobs_workspace.argtypes = [i32, i32, i32, P(i64)]
+        L.joint_logprobs.restype = ctypes.c_int
+        L.joint_logprobs.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.mx_quantize.restype = ctypes.c_int
+        L.mx_quantize.argtypes = [vp, i32, i64, i32, i32, vp, vp, vp]
+        L.mx_dequantize.restype = ctypes.c_int
+        L.mx_dequantize.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp]
+        L.joint_project_mx.restype = ctypes.c_int
+        L.joint_project_mx.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp]
         L.fusion_last_error.restype = ctypes.c_char_p
         L.fusion_last_error.argtypes = []
         L.fusion_device_status.restype = ctypes.c_int
@@ -341,6 +360,74 @@ def joint_project(A, W, bias, M, N, K, out, stream=None):
     bfloat16 CUDA tensors, bias and out float32 CUDA tensors."""
     _check(lib().joint_project(_ptr(A), _ptr(W), _ptr(bias), int(M), int(N), int(K), _ptr(out),
                                _stream(stream)))
+
+
+_DTYPES = None
+
+
+def _dtype(t) -> int:
+    """FUSION_F32 / FUSION_BF16 / FUSION_F16 of a tensor (anything else: -1, which the library refuses)."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+
+        _DTYPES = {torch.float32: FUSION_F32, torch.bfloat16: FUSION_BF16, torch.float16: FUSION_F16}
+    return _DTYPES.get(t.dtype, -1)
+
+
+def token_logprobs(logits, stride, T, S, B, V, tokens, parents, k, logp, entropy, lse, top_tokens=None, top_logp=None,
+                   stream=None):
+    """Same arguments as the C call, the dtype taken from logits; CUDA (HIP) tensors, float32 outputs."""
+    _check(lib().token_logprobs(_ptr(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V), _ptr(tokens),
+                                _ptr(parents), int(k), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_tokens),
+                                _ptr(top_logp), _stream(stream)))
+
+
+def token_logprobs_backward(logits, stride, T, S, B, V, tokens, parents, logp, entropy, lse, grad_logp, grad_entropy,
+                            grad_logits, grad_stride, stream=None):
+    """Same arguments as the C call, the dtype taken from logits (grad_logits has the same); CUDA (HIP) tensors."""
+    if grad_logits.dtype != logits.dtype:
+        raise ValueError("grad_logits must have the type of logits")
+    _check(lib().token_logprobs_backward(_ptr(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V),
+                                         _ptr(tokens), _ptr(parents), _ptr(logp), _ptr(entropy), _ptr(lse),
+                                         _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad_logits), int(grad_stride),
+                                         _stream(stream)))
+
+
+def joint_logprobs_workspace(M, V, K) -> int:
+    """float32 elements that joint_logprobs needs as its workspace for M = T * S * B rows."""
+    v = ctypes.c_int64()
+    _check(lib().joint_logprobs_workspace(int(M), int(V), int(K), ctypes.byref(v)))
+    return v.value
+
+
+def joint_logprobs(A, W, bias, K, T, S, B, V, tokens, parents, logp, entropy, lse, workspace, stream=None):
+    """Same arguments as the C call (the workspace's size is its tensor's); A and W bfloat16 (or int16 bit patterns)."""
+    _check(lib().joint_logprobs(_ptr(A), _ptr(W), _ptr(bias), int(K), int(T), int(S), int(B), int(V), _ptr(tokens),
+                                _ptr(parents), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(workspace),
+                                workspace.numel(), _stream(stream)))
+
+
+def mx_scale_stride(K) -> int:
+    """Scale bytes of a row of K values (FUSION_MX_SCALE_STRIDE)."""
+    return (int(K) // 32 + 7) // 8 * 8
+
+
+def mx_quantize(x, stride, R, K, q, scales, stream=None):
+    """Same arguments as the C call, the dtype taken from x; q [R, K // 2] and scales [R, mx_scale_stride(K)] uint8."""
+    _check(lib().mx_quantize(_ptr(x), _dtype(x), int(stride), int(R), int(K), _ptr(q), _ptr(scales), _stream(stream)))
+
+
+def mx_dequantize(q, scales, R, K, out, stride, stream=None):
+    """Same arguments as the C call, the dtype taken from out."""
+    _check(lib().mx_dequantize(_ptr(q), _ptr(scales), int(R), int(K), _ptr(out), _dtype(out), int(stride),
+                               _stream(stream)))
+
+
+def joint_project_mx(A, A_scales, W, W_scales, bias, M, N, K, out, stream=None):
+    """Same arguments as the C call; operands as mx_quantize writes them, bias and out float32 CUDA tensors."""
+    _check(lib().joint_project_mx(_ptr(A), _ptr(A_scales), _ptr(W), _ptr(W_scales), _ptr(bias), int(M), int(N), int(K),
+                                  _ptr(out), _stream(stream)))
 
 
 def fusion_device_status(stream=None) -> int:

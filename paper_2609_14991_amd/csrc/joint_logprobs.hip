@@ -1,0 +1,231 @@
+// Log probabilities of given tokens straight from the joint network's hidden
+// states: the projection of joint_proj.hip whose logits are never stored.
+//
+// A tile of logits, x = A W^T + bias, leaves as the softmax statistics of its rows
+// (wave_ops.h's Stat, 16 bytes a row instead of 4 a logit); a second kernel joins a
+// token's row over the column tiles and computes the token's own logit again, by
+// the same matrix instructions over the same steps of K, so that it is the value
+// which the statistics contain, to the bit.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "fusion_internal.h"
+#include "joint_tile.h"
+#include "wave_ops.h"
+
+namespace fusion {
+namespace {
+
+__device__ int32_t g_joint_score_status;
+
+// part: [column tiles][4][M] (m, ones, rest, u)
+template <class S>
+__global__ void __launch_bounds__(64 * S::waves, 2) joint_stat_kernel(const uint16_t *__restrict__ A,
+                                                                     const uint16_t *__restrict__ W,
+                                                                     const float *__restrict__ bias, int M, int N,
+                                                                     int K, int n_col_tiles, int map,
+                                                                     float *__restrict__ part) {
+  constexpr int kParts = S::WN * 4, kRow = kParts + 1;  // partial statistics of a row, and their row in LDS
+  static_assert(S::lds >= S::BM * kRow * 16, "LDS too small for the statistics");
+  __shared__ __align__(1024) unsigned char smem[S::lds];
+  int tr, tc;
+  tile_place(map, n_col_tiles, tr, tc);
+  const int bm = tr * S::BM, bn = tc * S::BN;
+  f32x4 acc[S::TM][S::TN];
+  Bf16Op op;
+  tile_product<S>(op, smem, A, W, M, N, K * 2, bm, bn, acc);
+
+  // lane l holds row l % 16 of each 16 x 16 tile, columns 4 * (l / 16) .. + 3
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, fc = lane >> 4;
+  const int wm = (wave / S::WN) * S::RM, wn = (wave % S::WN) * S::RN;
+  float bv[S::TN * 4];
+#pragma unroll
+  for (int j = 0; j < S::TN * 4; ++j) {
+    const int n = bn + wn + j / 4 * 16 + fc * 4 + j % 4;
+    bv[j] = n >= N ? -INFINITY : bias ? bias[n] : 0.0f;
+  }
+  wait_barrier<0>();  // every wave has read the last stage
+  f32x4 *stat = reinterpret_cast<f32x4 *>(smem);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    float x[S::TN * 4], top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < S::TN * 4; ++j) {
+      x[j] = acc[i][j / 4][j % 4] + bv[j];
+      top = fmaxf(top, x[j]);
+    }
+    Stat s = stat_none();
+    stat_take(s, x, top);
+    stat[(wm + i * 16 + fr) * kRow + (wave % S::WN) * 4 + fc] = f32x4{s.m, s.ones, s.rest, s.u};
+  }
+  __syncthreads();
+  for (int row = threadIdx.x; row < S::BM; row += 64 * S::waves) {
+    if (bm + row >= M) break;
+    Stat s = stat_none();
+#pragma unroll
+    for (int q = 0; q < kParts; ++q) {
+      const f32x4 v = stat[row * kRow + q];
+      stat_join(s, Stat{v[0], v[1], v[2], v[3]});
+    }
+    float *o = part + (int64_t)tc * 4 * M + bm + row;
+    o[0] = s.m;
+    o[M] = s.ones;
+    o[2 * (int64_t)M] = s.rest;
+    o[3 * (int64_t)M] = s.u;
+  }
+}
+
+struct JoinArgs {
+  const uint16_t *A, *W;
+  const float *bias, *part;
+  const int32_t *tokens, *parents;
+  float *logp, *entropy, *lse;
+  int32_t M, N, K, B, n_col_tiles;
+};
+
+// 16 tokens a wave
+__global__ void __launch_bounds__(256) joint_join_kernel(JoinArgs p) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, fc = lane >> 4;
+  const int64_t first = ((int64_t)blockIdx.x * 4 + wave) * 16;
+  if (first >= p.M) return;
+  const bool here = first + fr < p.M;
+  const int m = here ? (int)first + fr : 0;
+  const int64_t r = here ? row_of_token(p.parents, m, p.B) : -1;
+  const int tok = here && p.tokens ? p.tokens[m] : -1;
+  const bool bad_token = tok < -1 || tok >= p.N, scored = r >= 0 && tok >= 0 && !bad_token;
+
+  // the token's logit: of the 16 x 16 products of the wave's hidden states and
+  // weight rows, those on the diagonal
+  const __amdgpu_buffer_rsrc_t ra = rsrc(p.A, (uint32_t)((int64_t)p.M * p.K * 2));
+  const __amdgpu_buffer_rsrc_t rw = rsrc(p.W, (uint32_t)((int64_t)p.N * p.K * 2));
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (p.logp) {
+    const uint32_t oa = scored ? (uint32_t)(r * p.K * 2) : kOutside, ow = scored ? (uint32_t)((int64_t)tok * p.K * 2) : kOutside;
+#pragma unroll 4
+    for (int k = 0; k < p.K; k += 32) {
+      const uint32_t c = (uint32_t)(k + fc * 8) * 2;
+      const bool in = k + fc * 8 < p.K && scored;
+      const i32x4 a = __builtin_amdgcn_raw_buffer_load_b128(ra, in ? oa + c : kOutside, 0, 0);
+      const i32x4 w = __builtin_amdgcn_raw_buffer_load_b128(rw, in ? ow + c : kOutside, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, a), acc, 0, 0, 0);
+    }
+  }
+  const float at = (fr & 3) == 0 ? acc[0] : (fr & 3) == 1 ? acc[1] : (fr & 3) == 2 ? acc[2] : acc[3];
+  float x = __shfl(at, fr + 16 * (fr >> 2));
+  if (scored && p.bias) x = x + p.bias[tok];
+
+  Stat s = stat_none();
+  if (r >= 0)
+    for (int c = fc; c < p.n_col_tiles; c += 4) {
+      const float *o = p.part + (int64_t)c * 4 * p.M + r;
+      stat_join(s, Stat{o[0], o[p.M], o[2 * (int64_t)p.M], o[3 * (int64_t)p.M]});
+    }
+#pragma unroll
+  for (int d = 16; d <= 32; d *= 2)
+    stat_join(s, Stat{__shfl_xor(s.m, d), __shfl_xor(s.ones, d), __shfl_xor(s.rest, d), __shfl_xor(s.u, d)});
+  if (fc != 0 || !here) return;
+  const RowScore q = row_score(s);
+  const float nan = __int_as_float(0x7FC00000);
+  const bool bad = bad_token || r == -2;
+  if (p.logp) p.logp[m] = bad ? nan : !scored ? 0.0f : row_logp(q, x);
+  if (p.entropy) p.entropy[m] = r == -2 ? nan : q.entropy;
+  if (p.lse) p.lse[m] = r == -2 ? nan : q.lse;
+  if (bad) atomicOr(&g_joint_score_status, FUSION_STATUS_BAD_TOKEN);
+}
+
+constexpr TileShape<2, 4, 8, 4, 2> t256{};
+constexpr TileShape<2, 2, 4, 4, 2> t128{};
+constexpr TileShape<2, 2, 2, 4, 3> t64x128{};
+constexpr TileShape<2, 2, 2, 2, 4> t64{};
+constexpr TileShape<2, 2, 1, 2, 4> t32{};
+constexpr int64_t kCus = 256;
+
+template <class C>
+int64_t tiles(C, int M, int N) {
+  return (int64_t)((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
+}
+
+// the largest tile that fills the chip, as in joint_project
+template <class F>
+auto with_shape(int M, int N, F f) {
+  if (tiles(t256, M, N) >= 1000 && N > 128) return f(t256);
+  if (tiles(t128, M, N) > kCus) return f(t128);
+  if (tiles(t64x128, M, N) > kCus) return f(t64x128);
+  if (tiles(t64, M, N) > kCus) return f(t64);
+  return f(t32);
+}
+
+int64_t workspace(int M, int N) {
+  return with_shape(M, N, [&](auto c) { return (int64_t)((N + decltype(c)::BN - 1) / decltype(c)::BN) * 4 * M; });
+}
+
+int check_sizes(int64_t M, int32_t N, int32_t K) {
+  if (M < 0 || N < 1 || K < 8) return set_error(FUSION_E_ARG, "sizes out of range");
+  if (K % 8 != 0) return set_error(FUSION_E_UNSUPPORTED, "K must be a multiple of 8");
+  if (M > 0x7FFFFFF0ll / 2 / K || (int64_t)N * K * 2 > 0x7FFFFFF0ll)
+    return set_error(FUSION_E_UNSUPPORTED, "operand larger than 2 GiB: split the call along T");
+  return FUSION_OK;
+}
+
+}  // namespace
+
+int joint_score_status_take(int32_t *bits) {
+  int32_t v = 0, zero = 0;
+  hipError_t e = hipMemcpyFromSymbol(&v, HIP_SYMBOL(g_joint_score_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
+  if (e != hipSuccess) return hip_error(e, "hipMemcpyFromSymbol");
+  e = hipMemcpyToSymbol(HIP_SYMBOL(g_joint_score_status), &zero, sizeof(int32_t), 0, hipMemcpyHostToDevice);
+  if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
+  *bits = v;
+  return FUSION_OK;
+}
+
+}  // namespace fusion
+
+using namespace fusion;
+
+extern "C" int joint_logprobs_workspace(int32_t M, int32_t V, int32_t K, int64_t *floats) {
+  if (!floats) return set_error(FUSION_E_ARG, "NULL output");
+  const int rc = check_sizes(M, V, K);
+  if (rc != FUSION_OK) return rc;
+  *floats = workspace(M, V);
+  return FUSION_OK;
+}
+
+extern "C" int joint_logprobs(const uint16_t *A, const uint16_t *W, const float *bias, int32_t K, int32_t T, int32_t S,
+                              int32_t B, int32_t V, const int32_t *tokens, const int32_t *parents, float *logp,
+                              float *entropy, float *lse, float *workspace_, int64_t workspace_floats,
+                              hipStream_t stream) {
+  if (T < 0 || S < 0 || B < 1) return set_error(FUSION_E_ARG, "T, S or B out of range");
+  if (parents && B > FUSION_MAX_BEAM) return set_error(FUSION_E_UNSUPPORTED, "parents of more than FUSION_MAX_BEAM slots");
+  const int64_t H = (int64_t)S * B;
+  if (H > INT32_MAX || (H > 0 && T > INT32_MAX / H)) return set_error(FUSION_E_UNSUPPORTED, "more than 2^31 - 1 rows");
+  const int64_t M = T * H;
+  const int rc = check_sizes(M, V, K);
+  if (rc != FUSION_OK) return rc;
+  if (M == 0) return FUSION_OK;
+  if (!A || !W || !workspace_) return set_error(FUSION_E_ARG, "NULL operand or workspace");
+  if (((uintptr_t)A | (uintptr_t)W) % 16 != 0) return set_error(FUSION_E_ARG, "A and W must be 16-byte aligned");
+  if (logp && !tokens) return set_error(FUSION_E_ARG, "log probabilities of NULL tokens");
+  if (!logp && !entropy && !lse) return set_error(FUSION_E_ARG, "no output buffer");
+  if (workspace_floats < workspace((int)M, V)) return set_error(FUSION_E_ARG, "workspace too small");
+  const int nct = with_shape((int)M, V, [&](auto c) -> int {
+    using C = decltype(c);
+    const int cols = (V + C::BN - 1) / C::BN, rows = ((int)M + C::BM - 1) / C::BM;
+    if ((int64_t)cols * rows >= (1 << 23)) return -1;  // a launch holds fewer than 2^32 lanes
+    const int map = tile_map(rows, cols, tiles(t128, (int)M, V) > kCus, (int)M, V, (int64_t)V * K * 2);
+    hipLaunchKernelGGL((joint_stat_kernel<C>), dim3(cols * rows), dim3(64 * C::waves), 0, stream, A, W, bias, (int)M, V,
+                       K, cols, map, workspace_);
+    return cols;
+  });
+  if (nct < 0) return set_error(FUSION_E_UNSUPPORTED, "too many tiles: split the call along T");
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return hip_error(e, "joint statistics launch");
+  const JoinArgs p{A, W, bias, workspace_, logp ? tokens : nullptr, parents, logp, entropy, lse, (int32_t)M, V, K, B, nct};
+  hipLaunchKernelGGL(joint_join_kernel, dim3((unsigned)((M + 63) / 64)), dim3(256), 0, stream, p);
+  e = hipGetLastError();
+  return e == hipSuccess ? FUSION_OK : hip_error(e, "joint scoring launch");
+}

@@ -1,0 +1,464 @@
+// Log probabilities of the tokens that a decode chose, with the entropy of the
+// acoustic distribution they were chosen from and its best alternatives, and the
+// gradient of both with respect to the logits.
+//
+// Per token (slot h of frame t), x the logits row it was chosen on:
+//   m = max x, s = sum e^(x - m), u = sum (x - m) e^(x - m)
+//   lse = m + log s,  logp = (x_tok - m) - log s,  entropy = log s - u / s
+// and the k largest x - lse, ties to the lowest id.  Backward, p = e^(x - lse):
+//   dx_y = sum over the row's tokens of  g_logp (1[y = tok] - p_y)
+//                                      - g_entropy p_y (log p_y + entropy)
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "fusion_internal.h"
+#include "row_types.h"
+#include "wave_ops.h"
+
+namespace fusion {
+namespace {
+
+__device__ int32_t g_score_status;
+
+constexpr int kPer = 16;          // values a lane holds of a wave's chunk
+constexpr int kChunk = 64 * kPer;  // columns of a chunk
+constexpr int kList = 128;        // candidates a wave keeps
+
+// Column of value j of a lane's chunk
+template <class T>
+__device__ __forceinline__ int column(int base, int lane, int j) {
+  constexpr int n = Pack<T>::n;
+  return base + ((j / n) * 64 + lane) * n + j % n;
+}
+
+// Columns base .. base + 1023 of a row, -infinity past its end.  The pack that
+// straddles the end is read whole, ending at the row's last element, and shifted.
+template <class T>
+__device__ __forceinline__ void load_chunk(const T *row, int V, int base, int lane, float (&x)[kPer]) {
+  constexpr int n = Pack<T>::n;
+  if (V < n) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int c = column<T>(base, lane, j);
+      x[j] = c < V ? to_float(row[c]) : -INFINITY;
+    }
+    return;
+  }
+  Pack<T> p[kPer / n];
+#pragma unroll
+  for (int i = 0; i < kPer / n; ++i)
+    __builtin_memcpy(&p[i], row + min(base + (i * 64 + lane) * n, V - n), 16);
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) x[j] = to_float(p[j / n].v[j % n]);
+  if (base + kChunk > V) {
+#pragma unroll
+    for (int i = 0; i < kPer / n; ++i) {
+      const int shift = base + (i * 64 + lane) * n - (V - n);
+#pragma unroll
+      for (int b = 1; b < n; b *= 2)
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+          if (shift > 0 && (shift & b)) x[i * n + e] = e + b < n ? x[i * n + e + b] : -INFINITY;
+#pragma unroll
+      for (int e = 0; e < n; ++e)
+        if (shift >= n) x[i * n + e] = -INFINITY;
+    }
+  }
+}
+
+__device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
+
+// Orders a wave's own LDS writes before its later LDS reads by other lanes
+__device__ __forceinline__ void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
+// The k best (value descending, id ascending) of two entries a lane (-infinity:
+// none); lane r < k ends with the r-th, and with (-infinity, -1) where there is none
+__device__ __forceinline__ void pick_best(float v0, int i0, float v1, int i1, int k, int lane, float &v, int &id) {
+  v = -INFINITY;
+  id = -1;
+  for (int r = 0; r < k; ++r) {
+    const bool second = before(v1, i1, v0, i0);
+    const float b = second ? v1 : v0;
+    const float w = wave_max(b);
+    if (w == -INFINITY) break;
+    const int bi = wave_min(b == w ? (second ? i1 : i0) : INT_MAX);
+    if (lane == r) {
+      v = w;
+      id = bi;
+    }
+    if (v0 == w && i0 == bi) v0 = -INFINITY;
+    if (v1 == w && i1 == bi) v1 = -INFINITY;
+  }
+}
+
+// The candidates for the k best of the columns a wave has seen: a list in LDS,
+// of which at least k (or all there are) are no worse than (floor_v, floor_id),
+// and which holds everything that is better
+struct Best {
+  float *val;
+  int *id;
+  int count = 0;  // uniform
+  float floor_v = -INFINITY;
+  int floor_id = -1;
+};
+
+// keeps the k best of the list, in order
+__device__ __forceinline__ void best_shrink(Best &b, int k, int lane) {
+  wave_lds_sync();
+  const bool h0 = lane < b.count, h1 = lane + 64 < b.count;
+  const float v0 = h0 ? b.val[lane] : -INFINITY, v1 = h1 ? b.val[lane + 64] : -INFINITY;
+  const int i0 = h0 ? b.id[lane] : INT_MAX, i1 = h1 ? b.id[lane + 64] : INT_MAX;
+  float v;
+  int id;
+  pick_best(v0, i0, v1, i1, k, lane, v, id);
+  wave_lds_sync();
+  b.count = min(b.count, k);
+  if (lane < b.count) {
+    b.val[lane] = v;
+    b.id[lane] = id;
+  }
+  if (b.count == k) {
+    b.floor_v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), k - 1));
+    b.floor_id = __builtin_amdgcn_readlane(id, k - 1);
+  }
+  wave_lds_sync();
+}
+
+// the columns of one more chunk, which lie behind all seen before
+template <class T>
+__device__ __forceinline__ void best_take(Best &b, const float (&x)[kPer], float lane_max, int base, int k, int lane,
+                                          bool first) {
+  if (first) {
+    // the k-th largest of the lanes' maxima: at least k columns are no less
+    float left = lane_max;
+    for (int r = 0; r < k; ++r) {
+      b.floor_v = wave_max(left);
+      if (b.floor_v == -INFINITY) break;
+      if (lane == __builtin_ctzll(__ballot(left == b.floor_v))) left = -INFINITY;
+    }
+    b.floor_id = b.floor_v == -INFINITY ? -1 : INT_MAX;
+  } else {
+    b.floor_id = -1;  // a column behind the k that are no less than the floor has to exceed it
+    if (!__ballot(lane_max > b.floor_v)) return;
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int c = column<T>(base, lane, j);
+    bool in = before(x[j], c, b.floor_v, b.floor_id);
+    unsigned long long mask = __ballot(in);
+    if (!mask) continue;
+    if (b.count + __popcll(mask) > kList) {
+      best_shrink(b, k, lane);
+      in = before(x[j], c, b.floor_v, b.floor_id);
+      mask = __ballot(in);
+    }
+    if (in) {
+      const int at = b.count + __builtin_amdgcn_mbcnt_hi(mask >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+      b.val[at] = x[j];
+      b.id[at] = c;
+    }
+    b.count += __popcll(mask);
+  }
+}
+
+struct ScoreArgs {
+  const void *logits;
+  const int32_t *tokens, *parents;
+  float *logp, *entropy, *lse, *top_logp;
+  int32_t *top_tokens;
+  int64_t stride;
+  int32_t M, B, V, k;
+};
+
+// W waves a token: 4 tokens a workgroup of 256 lanes with one wave each, else one
+template <class T, int W>
+__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs p) {
+  constexpr int kWaves = W == 1 ? 4 : W;
+  __shared__ float s_val[kWaves][kList];
+  __shared__ int s_id[kWaves][kList];
+  __shared__ Stat s_stat[kWaves];
+  __shared__ int s_count[kWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t token_at = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  if (token_at >= p.M) return;  // whole waves, and with W > 1 none
+  const int m = (int)token_at;
+  const int64_t r = row_of_token(p.parents, m, p.B);
+  const int tok = p.tokens ? p.tokens[m] : -1;
+  const bool bad_token = tok < -1 || tok >= p.V;
+  const bool dead = r < 0;
+  const T *row = static_cast<const T *>(p.logits) + (dead ? 0 : r) * p.stride;
+  float x_tok = 0.0f;
+  if (!dead && tok >= 0 && !bad_token) x_tok = to_float(row[tok]);
+  Stat s = stat_none();
+  Best b;
+  b.val = s_val[wave];
+  b.id = s_id[wave];
+  if (!dead) {
+    bool first = true;
+    for (int base = (W == 1 ? 0 : wave) * kChunk; base < p.V; base += W * kChunk) {
+      float x[kPer];
+      load_chunk(row, p.V, base, lane, x);
+      float top = x[0];
+#pragma unroll
+      for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[j]);
+      top = fmaxf(top, -INFINITY);  // of NaNs alone
+      if (p.k) best_take<T>(b, x, top, base, p.k, lane, first);
+      stat_take(s, x, top);
+      first = false;
+    }
+  }
+  stat_wave(s);
+  if (p.k) best_shrink(b, p.k, lane);
+  float v = -INFINITY;
+  int id = -1;
+  if (W > 1) {
+    if (lane == 0) {
+      s_stat[wave] = s;
+      s_count[wave] = b.count;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    s = lane < W ? s_stat[lane] : stat_none();
+    stat_wave(s);
+    if (p.k) {
+      float ev[2];
+      int ei[2];
+      for (int q = 0; q < 2; ++q) {
+        const int w = (lane + 64 * q) / FUSION_MAX_K, at = (lane + 64 * q) % FUSION_MAX_K;
+        const bool has = w < W && at < s_count[w < W ? w : 0];
+        ev[q] = has ? s_val[w][at] : -INFINITY;
+        ei[q] = has ? s_id[w][at] : INT_MAX;
+      }
+      pick_best(ev[0], ei[0], ev[1], ei[1], p.k, lane, v, id);
+    }
+  } else if (p.k && lane < b.count) {
+    v = b.val[lane];
+    id = b.id[lane];
+  }
+  const RowScore q = row_score(s);
+  const float nan = __int_as_float(0x7FC00000);
+  const bool bad = bad_token || r == -2;
+  if (lane < p.k) {
+    const bool none = dead || q.bad || id < 0;
+    p.top_tokens[(int64_t)m * p.k + lane] = none ? -1 : id;
+    p.top_logp[(int64_t)m * p.k + lane] = r == -2 || (!dead && q.bad) ? nan : none ? -INFINITY : row_logp(q, v);
+  }
+  if (lane == 0) {
+    if (p.logp) p.logp[m] = bad ? nan : dead || tok < 0 ? 0.0f : row_logp(q, x_tok);
+    if (p.entropy) p.entropy[m] = r == -2 ? nan : q.entropy;
+    if (p.lse) p.lse[m] = r == -2 ? nan : q.lse;
+    if (bad) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
+  }
+}
+
+struct GradArgs {
+  const void *logits;
+  const int32_t *tokens, *parents;
+  const float *logp, *entropy, *lse, *g_logp, *g_entropy;
+  void *grad;
+  int64_t stride, g_stride;
+  int32_t M, B, V;
+};
+
+// a wave a row and chunk of 1024 columns
+template <class T>
+__global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
+  constexpr int n = Pack<T>::n;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunks = (p.V + kChunk - 1) / kChunk;
+  const int64_t job = (int64_t)blockIdx.x * 4 + wave;
+  if (job >= (int64_t)p.M * chunks) return;
+  const int r = (int)(job / chunks), base = (int)(job % chunks) * kChunk;
+  const T *row = static_cast<const T *>(p.logits) + r * p.stride;
+  T *out = static_cast<T *>(p.grad) + r * p.g_stride;
+  const bool whole = base + kChunk <= p.V;
+
+  // The tokens chosen on this row: lane i looks at slot i of the row's stream
+  const int slots = p.parents ? p.B : 1, first = p.parents ? r / p.B * p.B : r;
+  const int at = first + lane;
+  bool mine = lane < slots, bad = false;
+  if (mine && p.parents) {
+    const int par = p.parents[at];
+    bad = par < -1 || par >= p.B;
+    mine = par == r - first;
+  }
+  int tok = -1;
+  float gl = 0.0f, ge = 0.0f, lp_tok = 0.0f;
+  if (mine) {
+    if (p.tokens) tok = p.tokens[at];
+    if (tok < -1 || tok >= p.V) {
+      bad = true;
+      tok = -1;
+    }
+    if (tok >= 0 && p.g_logp) {
+      gl = p.g_logp[at];
+      lp_tok = p.logp[at];
+    } else {
+      tok = -1;
+    }
+    if (p.g_entropy) ge = p.g_entropy[at];
+  }
+  const unsigned long long any = __ballot(mine);
+  if (__ballot(bad) && lane == 0) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
+  float lse = 0.0f, H = 0.0f;
+  if (any) {
+    const int q = first + __builtin_ctzll(any);
+    lse = p.lse[q];
+    if (p.g_entropy) H = p.entropy[q];
+  }
+  const float GL = wave_add(gl), GE = wave_add(ge);
+  const bool nothing = !any || lse == -INFINITY;  // an empty row's outputs are constant
+
+  float x[kPer];
+  if (nothing) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) x[j] = 0.0f;
+  } else {
+    if (whole) {
+      Pack<T> q[kPer / n];
+#pragma unroll
+      for (int i = 0; i < kPer / n; ++i) __builtin_memcpy(&q[i], row + base + (i * 64 + lane) * n, 16);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) x[j] = to_float(q[j / n].v[j % n]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const int c = column<T>(base, lane, j);
+        x[j] = c < p.V ? to_float(row[c]) : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const float lp = x[j] - lse, e = exp_of(lp);
+      x[j] = -e * (GL + GE * (fmaxf(lp, kFar) + H));
+    }
+    // the tokens' own columns, from their log probabilities: 1 - p is lost in x - lse where p is near 1
+    unsigned long long todo = __ballot(tok >= base && tok < base + kChunk);
+    while (todo) {
+      const int i = __builtin_ctzll(todo);
+      const int y = __builtin_amdgcn_readlane(tok, i);
+      const float lp = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lp_tok), i));
+      const bool same = tok == y;
+      const float own = wave_add(same ? gl : 0.0f), others = wave_add(same ? 0.0f : gl);
+      const float e = exp_of(lp), g = own * -expm1f(lp) - e * (others + GE * (fmaxf(lp, kFar) + H));
+#pragma unroll
+      for (int j = 0; j < kPer; ++j)
+        if (column<T>(base, lane, j) == y) x[j] = g;
+      todo &= ~__ballot(same);
+    }
+  }
+  if (whole) {
+    Pack<T> q[kPer / n];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) from_float(x[j], q[j / n].v[j % n]);
+#pragma unroll
+    for (int i = 0; i < kPer / n; ++i) __builtin_memcpy(out + base + (i * 64 + lane) * n, &q[i], 16);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int c = column<T>(base, lane, j);
+      if (c < p.V) from_float(x[j], out[c]);
+    }
+  }
+}
+
+}  // namespace
+
+// the status bits of the scoring kernels, cleared (fusion_device_status merges them)
+int score_status_take(int32_t *bits) {
+  int32_t v = 0, zero = 0;
+  hipError_t e = hipMemcpyFromSymbol(&v, HIP_SYMBOL(g_score_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
+  if (e != hipSuccess) return hip_error(e, "hipMemcpyFromSymbol");
+  e = hipMemcpyToSymbol(HIP_SYMBOL(g_score_status), &zero, sizeof(int32_t), 0, hipMemcpyHostToDevice);
+  if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
+  *bits = v;
+  return FUSION_OK;
+}
+
+namespace {
+constexpr int64_t kMaxRows = (1 << 24) - 1;
+// the checks that scoring and its gradient share
+int check_rows(int32_t dtype, int64_t stride, int32_t T, int32_t S, int32_t B, int32_t V, const void *parents) {
+  if (dtype != FUSION_F32 && dtype != FUSION_BF16 && dtype != FUSION_F16) return set_error(FUSION_E_ARG, "unknown dtype");
+  if (T < 0 || S < 0 || B < 1) return set_error(FUSION_E_ARG, "T, S or B out of range");
+  if (parents && B > FUSION_MAX_BEAM) return set_error(FUSION_E_UNSUPPORTED, "parents of more than FUSION_MAX_BEAM slots");
+  if (V < 1 || V > FUSION_MAX_SCORED_VOCAB) return set_error(FUSION_E_ARG, "V out of range");
+  if (stride < V) return set_error(FUSION_E_ARG, "rows overlap: stride below V");
+  const int64_t H = (int64_t)S * B;
+  // (a launch holds fewer than 2^32 lanes)
+  if (H > kMaxRows || (H > 0 && T > kMaxRows / H)) return set_error(FUSION_E_UNSUPPORTED, "more than 2^24 - 1 rows");
+  // the last row's end within a 63-bit byte offset
+  if (stride > (INT64_MAX >> 3) / (H > 0 && T > 0 ? T * H : 1)) return set_error(FUSION_E_ARG, "stride out of range");
+  return FUSION_OK;
+}
+}  // namespace
+
+}  // namespace fusion
+
+using namespace fusion;
+
+extern "C" int token_logprobs(const void *logits, int32_t dtype, int64_t stride, int32_t T, int32_t S, int32_t B,
+                              int32_t V, const int32_t *tokens, const int32_t *parents, int32_t k, float *logp,
+                              float *entropy, float *lse, int32_t *top_tokens, float *top_logp, hipStream_t stream) {
+  const int rc = check_rows(dtype, stride, T, S, B, V, parents);
+  if (rc != FUSION_OK) return rc;
+  if (k < 0 || k > FUSION_MAX_K) return set_error(FUSION_E_ARG, "k out of range");
+  const int64_t M = (int64_t)T * S * B;
+  if (M == 0) return FUSION_OK;
+  if (!logits) return set_error(FUSION_E_ARG, "NULL logits");
+  if ((uintptr_t)logits % (dtype == FUSION_F32 ? 4 : 2) != 0) return set_error(FUSION_E_ARG, "misaligned logits");
+  if (logp && !tokens) return set_error(FUSION_E_ARG, "log probabilities of NULL tokens");
+  if (k > 0 && (!top_tokens || !top_logp)) return set_error(FUSION_E_ARG, "NULL buffer for the alternatives");
+  if (!logp && !entropy && !lse && k == 0) return set_error(FUSION_E_ARG, "no output buffer");
+  const ScoreArgs p{logits, logp ? tokens : nullptr, parents, logp, entropy, lse, top_logp, top_tokens, stride, (int32_t)M,
+                    B, V, k};
+  auto go = [&](auto type) {
+    using T_ = decltype(type);
+    if (M >= 4096 || V <= kChunk)
+      hipLaunchKernelGGL((score_kernel<T_, 1>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, stream, p);
+    else if (M >= 1024 || V <= 4 * kChunk)
+      hipLaunchKernelGGL((score_kernel<T_, 4>), dim3((unsigned)M), dim3(256), 0, stream, p);
+    else
+      hipLaunchKernelGGL((score_kernel<T_, 16>), dim3((unsigned)M), dim3(1024), 0, stream, p);
+  };
+  if (dtype == FUSION_F32) go(float{});
+  else if (dtype == FUSION_BF16) go(Brain{});
+  else go(Half{});
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FUSION_OK : hip_error(e, "token scoring launch");
+}
+
+extern "C" int token_logprobs_backward(const void *logits, int32_t dtype, int64_t stride, int32_t T, int32_t S, int32_t B,
+                                       int32_t V, const int32_t *tokens, const int32_t *parents, const float *logp,
+                                       const float *entropy, const float *lse, const float *grad_logp,
+                                       const float *grad_entropy, void *grad_logits, int64_t grad_stride,
+                                       hipStream_t stream) {
+  const int rc = check_rows(dtype, stride, T, S, B, V, parents);
+  if (rc != FUSION_OK) return rc;
+  if (check_rows(dtype, grad_stride, T, S, B, V, parents) != FUSION_OK)
+    return set_error(FUSION_E_ARG, "gradient rows overlap or their stride is out of range");
+  const int64_t M = (int64_t)T * S * B;
+  if (M == 0) return FUSION_OK;
+  if (!logits || !grad_logits || !lse) return set_error(FUSION_E_ARG, "NULL logits, gradient or lse");
+  if (((uintptr_t)logits | (uintptr_t)grad_logits) % (dtype == FUSION_F32 ? 4 : 2) != 0)
+    return set_error(FUSION_E_ARG, "misaligned logits or gradient");
+  if (!grad_logp && !grad_entropy) return set_error(FUSION_E_ARG, "no incoming gradient");
+  if (grad_logp && (!tokens || !logp)) return set_error(FUSION_E_ARG, "gradient of the log probabilities without tokens or logp");
+  if (grad_entropy && !entropy) return set_error(FUSION_E_ARG, "gradient of the entropy without entropy");
+  if (logits == grad_logits && stride != grad_stride) return set_error(FUSION_E_ARG, "in place with another stride");
+  const int64_t blocks = (M * ((V + kChunk - 1) / kChunk) + 3) / 4;
+  if (blocks >= 1 << 24) return set_error(FUSION_E_UNSUPPORTED, "too many rows: split the call along T");
+  const GradArgs p{logits, tokens, parents, logp, entropy, lse, grad_logp, grad_entropy, grad_logits, stride, grad_stride,
+                   (int32_t)M, B, V};
+  const dim3 grid((unsigned)blocks), block(256);
+  if (dtype == FUSION_F32) hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, p);
+  else if (dtype == FUSION_BF16) hipLaunchKernelGGL(grad_kernel<Brain>, grid, block, 0, stream, p);
+  else hipLaunchKernelGGL(grad_kernel<Half>, grid, block, 0, stream, p);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? FUSION_OK : hip_error(e, "token scoring gradient launch");
+}

@@ -1,0 +1,142 @@
+// Wave-wide reductions and row access shared by the scoring kernels
+// (logprobs.hip, joint_logprobs.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <climits>
+#include <cstdint>
+
+namespace fusion {
+
+constexpr float kLog2e = 1.4426950408889634f;
+// stands for -infinity in x - max: e^it is 0, and 0 times it is 0 and not NaN
+constexpr float kFar = -1e4f;
+
+// one step of a reduction: the neighbour's value under a DPP pattern
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int wave_move(int ident, int v) {
+  return __builtin_amdgcn_update_dpp(ident, v, CTRL, ROWS, 0xF, false);
+}
+// op over the 64 lanes, the result in every lane: quads, half rows and rows of 16
+// lanes, then row 0 into 1 and 2 into 3, then the lower half into the upper
+template <class F>
+__device__ __forceinline__ int wave_reduce(int ident, int v, F op) {
+  v = op(v, wave_move<0xB1, 0xF>(ident, v));
+  v = op(v, wave_move<0x4E, 0xF>(ident, v));
+  v = op(v, wave_move<0x141, 0xF>(ident, v));
+  v = op(v, wave_move<0x140, 0xF>(ident, v));
+  v = op(v, wave_move<0x142, 0xA>(ident, v));
+  v = op(v, wave_move<0x143, 0xC>(ident, v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return __int_as_float(wave_reduce(__float_as_int(-INFINITY), __float_as_int(x), [](int a, int b) {
+    return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b)));
+  }));
+}
+__device__ __forceinline__ float wave_add(float x) {
+  return __int_as_float(wave_reduce(0, __float_as_int(x), [](int a, int b) {
+    return __float_as_int(__int_as_float(a) + __int_as_float(b));
+  }));
+}
+__device__ __forceinline__ int wave_min(int x) {
+  return wave_reduce(INT_MAX, x, [](int a, int b) { return min(a, b); });
+}
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// Softmax statistics of a set of values: their maximum m, how many equal it, the
+// sum of e^(x - m) over the others and the sum of (x - m) e^(x - m).  The ones are
+// counted apart from the sum because where one value holds nearly all of the
+// probability, its log probability is -log(1 + rest) and the entropy is of the
+// size of the rest, which 1 + rest in fp32 would round off.
+// A NaN or +infinity among the values makes `rest` NaN and stays there.
+struct Stat {
+  float m, ones, rest, u;
+};
+__device__ __forceinline__ Stat stat_none() { return Stat{-INFINITY, 0.0f, 0.0f, 0.0f}; }
+
+// the same set's statistics relative to a maximum M >= s.m
+__device__ __forceinline__ void stat_lift(Stat &s, float M) {
+  const float base = M == -INFINITY ? 0.0f : M;
+  const float d = fmaxf(s.m - base, kFar), f = exp_of(d), all = s.ones + s.rest;
+  if (s.m != M) {
+    s.u = f * (s.u + d * all);
+    s.rest = f * all;
+    s.ones = 0.0f;
+    s.m = M;
+  }
+}
+
+// `n` more values; lane_max is their maximum
+template <int n>
+__device__ __forceinline__ void stat_take(Stat &s, const float (&x)[n], float lane_max) {
+  stat_lift(s, fmaxf(s.m, lane_max));
+  const float base = s.m == -INFINITY ? 0.0f : s.m;
+#pragma unroll
+  for (int j = 0; j < n; ++j) {
+    const float d = x[j] - base, e = exp_of(d);
+    s.ones += d == 0.0f ? 1.0f : 0.0f;
+    s.rest += d == 0.0f ? 0.0f : e;
+    s.u = fmaf(fmaxf(d, kFar), e, s.u);
+  }
+}
+
+// two sets' statistics as one
+__device__ __forceinline__ void stat_join(Stat &s, Stat o) {
+  const float M = fmaxf(s.m, o.m);
+  stat_lift(s, M);
+  stat_lift(o, M);
+  s.ones += o.ones;
+  s.rest += o.rest;
+  s.u += o.u;
+}
+
+// the 64 lanes' statistics as one, in every lane
+__device__ __forceinline__ void stat_wave(Stat &s) {
+  stat_lift(s, wave_max(s.m));
+  s.ones = wave_add(s.ones);
+  s.rest = wave_add(s.rest);
+  s.u = wave_add(s.u);
+}
+
+// what a finished set's statistics say
+struct RowScore {
+  float m, log_s, lse, entropy;
+  bool empty, bad;  // nothing above -infinity; a NaN or +infinity in the row
+};
+__device__ __forceinline__ RowScore row_score(const Stat &s) {
+  RowScore r;
+  const float all = s.ones + s.rest;
+  r.bad = !(all < INFINITY);
+  r.empty = all == 0.0f;
+  r.m = s.m;
+  r.log_s = log1pf((s.ones - 1.0f) + s.rest);
+  r.lse = s.m + r.log_s;
+  r.entropy = r.log_s - s.u / all;
+  if (r.empty) {
+    r.log_s = 0.0f;
+    r.lse = -INFINITY;
+    r.entropy = 0.0f;
+  }
+  if (r.bad) r.log_s = r.lse = r.entropy = __int_as_float(0x7FC00000);
+  return r;
+}
+// log probability of a value of the row
+__device__ __forceinline__ float row_logp(const RowScore &r, float x) {
+  return r.empty ? -INFINITY : (x - r.m) - r.log_s;
+}
+
+// Where the token of slot b of stream s at frame t was chosen: the row of its
+// parent slot, or its own without parents; -1 for a dead slot, -2 for a parent
+// outside the beam
+__device__ __forceinline__ int64_t row_of_token(const int32_t *parents, int32_t m, int32_t B) {
+  if (!parents) return m;
+  const int32_t p = parents[m];
+  if (p == -1) return -1;
+  if (p < 0 || p >= B) return -2;
+  return (int64_t)(m / B) * B + p;
+}
+
+}  // namespace fusion
