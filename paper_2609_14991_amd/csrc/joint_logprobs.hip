@@ -1,7 +1,7 @@
 // Log probabilities of given tokens straight from the joint network's hidden
 // states: the projection of joint_proj.hip whose logits are never stored.
 //
-// A tile of logits, x = A W^T + bias, leaves as the softmax statistics of its rows
+// A tile of logits, x = bias + A W^T, leaves as the softmax statistics of its rows
 // (wave_ops.h's Stat, 16 bytes a row instead of 4 a logit); a second kernel joins a
 // token's row over the column tiles and computes the token's own logit again, by
 // the same matrix instructions over the same steps of K, so that it is the value
@@ -20,61 +20,97 @@ namespace {
 
 __device__ int32_t g_joint_score_status;
 
-// part: [column tiles][4][M] (m, ones, rest, u)
+// Statistics of a row's 16 TN logits in four lanes (l, l ^ 16, l ^ 32, l ^ 48), in
+// all of them.  Four operations a logit, the exponential among them; the maxima are
+// counted as one, which the sum less 1 then holds to 1e-5 unless next to nothing
+// else is in it.  Where that is so (one logit far above the row's others) or a
+// logit is -infinity (0 times it is NaN), once more with care.
+template <int TN>
+__device__ __forceinline__ Stat tile_row_stat(const f32x4 (&x)[TN]) {
+  float top = x[0][0], low = x[0][0];
+#pragma unroll
+  for (int j = 0; j < 4 * TN; ++j) {
+    top = fmaxf(top, x[j / 4][j % 4]);
+    low = fminf(low, x[j / 4][j % 4]);
+  }
+  Stat s{across_rows(top, [](float a, float b) { return fmaxf(a, b); }), 1.0f, 0.0f, 0.0f};
+  const float shift = -s.m * kLog2e;
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4 * TN; ++j) {
+    const float t = fmaf(x[j / 4][j % 4], kLog2e, shift), e = __builtin_amdgcn_exp2f(t);
+    sum += e;
+    s.u = fmaf(t, e, s.u);
+  }
+  const auto add = [](float a, float b) { return a + b; };
+  s.rest = across_rows(sum, add) - 1.0f;
+  s.u = across_rows(s.u * kLn2, add);
+  if (__ballot(low == -INFINITY || s.rest < 0.0625f)) {
+    float v[4 * TN];
+#pragma unroll
+    for (int j = 0; j < 4 * TN; ++j) v[j] = x[j / 4][j % 4];
+    Stat c = stat_none();
+    stat_take(c, v, s.m);
+    s = Stat{s.m, across_rows(c.ones, add), across_rows(c.rest, add), across_rows(c.u, add)};
+  }
+  return s;
+}
+
+struct StatArgs {
+  const uint16_t *A, *W;
+  const float *bias;
+  float *part;  // [column tiles][4][M] (m, ones, rest, u)
+  int M, N, K, n_col_tiles, map;
+};
+
 template <class S>
-__global__ void __launch_bounds__(64 * S::waves, 2) joint_stat_kernel(const uint16_t *__restrict__ A,
-                                                                     const uint16_t *__restrict__ W,
-                                                                     const float *__restrict__ bias, int M, int N,
-                                                                     int K, int n_col_tiles, int map,
-                                                                     float *__restrict__ part) {
-  constexpr int kParts = S::WN * 4, kRow = kParts + 1;  // partial statistics of a row, and their row in LDS
-  static_assert(S::lds >= S::BM * kRow * 16, "LDS too small for the statistics");
+__global__ void __launch_bounds__(64 * S::waves, 2) joint_stat_kernel(StatArgs p) {
+  static_assert(S::lds >= S::BM * S::WN * 16, "LDS too small for the statistics");
   __shared__ __align__(1024) unsigned char smem[S::lds];
   int tr, tc;
-  tile_place(map, n_col_tiles, tr, tc);
+  tile_place(p.map, p.n_col_tiles, tr, tc);
   const int bm = tr * S::BM, bn = tc * S::BN;
-  f32x4 acc[S::TM][S::TN];
-  Bf16Op op;
-  tile_product<S>(op, smem, A, W, M, N, K * 2, bm, bn, acc);
-
-  // lane l holds row l % 16 of each 16 x 16 tile, columns 4 * (l / 16) .. + 3
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fc = lane >> 4;
   const int wm = (wave / S::WN) * S::RM, wn = (wave % S::WN) * S::RN;
-  float bv[S::TN * 4];
+  // the sums start at the bias, at -infinity in columns past N: lane l holds row
+  // l % 16 of each 16 x 16 tile, columns 4 * (l / 16) .. + 3
+  f32x4 acc[S::TM][S::TN];
 #pragma unroll
-  for (int j = 0; j < S::TN * 4; ++j) {
-    const int n = bn + wn + j / 4 * 16 + fc * 4 + j % 4;
-    bv[j] = n >= N ? -INFINITY : bias ? bias[n] : 0.0f;
+  for (int j = 0; j < S::TN; ++j) {
+    f32x4 b;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int n = bn + wn + j * 16 + fc * 4 + r;
+      b[r] = n >= p.N ? -INFINITY : p.bias ? p.bias[n] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) acc[i][j] = b;
   }
+  Bf16Op op;
+  tile_product<S>(op, smem, p.A, p.W, p.M, p.N, p.K * 2, bm, bn, acc);
+
   wait_barrier<0>();  // every wave has read the last stage
   f32x4 *stat = reinterpret_cast<f32x4 *>(smem);
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
-    float x[S::TN * 4], top = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < S::TN * 4; ++j) {
-      x[j] = acc[i][j / 4][j % 4] + bv[j];
-      top = fmaxf(top, x[j]);
-    }
-    Stat s = stat_none();
-    stat_take(s, x, top);
-    stat[(wm + i * 16 + fr) * kRow + (wave % S::WN) * 4 + fc] = f32x4{s.m, s.ones, s.rest, s.u};
+    const Stat s = tile_row_stat<S::TN>(acc[i]);
+    if (fc == 0) stat[(wm + i * 16 + fr) * S::WN + wave % S::WN] = f32x4{s.m, s.ones, s.rest, s.u};
   }
   __syncthreads();
   for (int row = threadIdx.x; row < S::BM; row += 64 * S::waves) {
-    if (bm + row >= M) break;
+    if (bm + row >= p.M) break;
     Stat s = stat_none();
 #pragma unroll
-    for (int q = 0; q < kParts; ++q) {
-      const f32x4 v = stat[row * kRow + q];
+    for (int q = 0; q < S::WN; ++q) {
+      const f32x4 v = stat[row * S::WN + q];
       stat_join(s, Stat{v[0], v[1], v[2], v[3]});
     }
-    float *o = part + (int64_t)tc * 4 * M + bm + row;
+    float *o = p.part + (int64_t)tc * 4 * p.M + bm + row;
     o[0] = s.m;
-    o[M] = s.ones;
-    o[2 * (int64_t)M] = s.rest;
-    o[3 * (int64_t)M] = s.u;
+    o[p.M] = s.ones;
+    o[2 * (int64_t)p.M] = s.rest;
+    o[3 * (int64_t)p.M] = s.u;
   }
 }
 
@@ -86,47 +122,76 @@ struct JoinArgs {
   int32_t M, N, K, B, n_col_tiles;
 };
 
-// 16 tokens a wave
+// A wave computes the logits of 16 tokens; `split` waves join the column tiles of
+// their rows, four lanes a row each.  One wave a group for many tokens; four where
+// there are few and each waits for its loads alone (256 tokens of 64 column tiles:
+// 4.6 us, 12 with one wave and its loads one after the other)
+template <int split>
 __global__ void __launch_bounds__(256) joint_join_kernel(JoinArgs p) {
+  static_assert(split == 1 || split == 4, "one wave a group of 16 tokens, or the workgroup");
+  constexpr int groups = 4 / split;  // of 16 tokens a workgroup
+  __shared__ f32x4 s_part[4][16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fc = lane >> 4;
-  const int64_t first = ((int64_t)blockIdx.x * 4 + wave) * 16;
-  if (first >= p.M) return;
-  const bool here = first + fr < p.M;
-  const int m = here ? (int)first + fr : 0;
+  const int64_t at = ((int64_t)blockIdx.x * groups + wave / split) * 16 + fr;
+  const bool here = at < p.M;
+  const int m = here ? (int)at : 0;
   const int64_t r = here ? row_of_token(p.parents, m, p.B) : -1;
   const int tok = here && p.tokens ? p.tokens[m] : -1;
   const bool bad_token = tok < -1 || tok >= p.N, scored = r >= 0 && tok >= 0 && !bad_token;
 
-  // the token's logit: of the 16 x 16 products of the wave's hidden states and
-  // weight rows, those on the diagonal
-  const __amdgpu_buffer_rsrc_t ra = rsrc(p.A, (uint32_t)((int64_t)p.M * p.K * 2));
-  const __amdgpu_buffer_rsrc_t rw = rsrc(p.W, (uint32_t)((int64_t)p.N * p.K * 2));
-  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (p.logp) {
-    const uint32_t oa = scored ? (uint32_t)(r * p.K * 2) : kOutside, ow = scored ? (uint32_t)((int64_t)tok * p.K * 2) : kOutside;
-#pragma unroll 4
-    for (int k = 0; k < p.K; k += 32) {
-      const uint32_t c = (uint32_t)(k + fc * 8) * 2;
-      const bool in = k + fc * 8 < p.K && scored;
-      const i32x4 a = __builtin_amdgcn_raw_buffer_load_b128(ra, in ? oa + c : kOutside, 0, 0);
-      const i32x4 w = __builtin_amdgcn_raw_buffer_load_b128(rw, in ? ow + c : kOutside, 0, 0);
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, a), acc, 0, 0, 0);
+  Stat s = stat_none();
+  if (r >= 0) {
+    constexpr int kAhead = 4;
+    for (int c = wave % split * 4 + fc; c < p.n_col_tiles; c += 4 * split * kAhead) {
+      Stat v[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const float *o = p.part + (int64_t)min(c + 4 * split * q, p.n_col_tiles - 1) * 4 * p.M + r;
+        v[q] = Stat{o[0], o[p.M], o[2 * (int64_t)p.M], o[3 * (int64_t)p.M]};
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q)
+        if (c + 4 * split * q < p.n_col_tiles) stat_join(s, v[q]);
     }
   }
-  const float at = (fr & 3) == 0 ? acc[0] : (fr & 3) == 1 ? acc[1] : (fr & 3) == 2 ? acc[2] : acc[3];
-  float x = __shfl(at, fr + 16 * (fr >> 2));
-  if (scored && p.bias) x = x + p.bias[tok];
+  s = stat_across(s);
+  if (split > 1) {
+    if (fc == 0) s_part[wave][fr] = f32x4{s.m, s.ones, s.rest, s.u};
+    __syncthreads();
+    if (wave != 0) return;
+    const f32x4 v = s_part[fc][fr];
+    s = stat_across(Stat{v[0], v[1], v[2], v[3]});
+  }
 
-  Stat s = stat_none();
-  if (r >= 0)
-    for (int c = fc; c < p.n_col_tiles; c += 4) {
-      const float *o = p.part + (int64_t)c * 4 * p.M + r;
-      stat_join(s, Stat{o[0], o[p.M], o[2 * (int64_t)p.M], o[3 * (int64_t)p.M]});
-    }
+  // the token's logit: of the 16 x 16 products of the wave's hidden states and
+  // weight rows, those on the diagonal
+  float x = 0.0f;
+  if (p.logp) {
+    const __amdgpu_buffer_rsrc_t ra = rsrc(p.A, (uint32_t)((int64_t)p.M * p.K * 2));
+    const __amdgpu_buffer_rsrc_t rw = rsrc(p.W, (uint32_t)((int64_t)p.N * p.K * 2));
+    const float b = scored && p.bias ? p.bias[tok] : 0.0f;
+    f32x4 acc = {b, b, b, b};
+    const uint32_t oa = scored ? (uint32_t)(r * p.K * 2) : kOutside, ow = scored ? (uint32_t)((int64_t)tok * p.K * 2) : kOutside;
+    // the loads of 10 steps at a time: one step after the other they would be most of the time
+    constexpr int kSteps = 10;
+    for (int k = 0; k < p.K; k += 32 * kSteps) {
+      i32x4 a[kSteps], w[kSteps];
 #pragma unroll
-  for (int d = 16; d <= 32; d *= 2)
-    stat_join(s, Stat{__shfl_xor(s.m, d), __shfl_xor(s.ones, d), __shfl_xor(s.rest, d), __shfl_xor(s.u, d)});
+      for (int q = 0; q < kSteps; ++q) {
+        const int e = k + q * 32 + fc * 8;
+        const bool in = e < p.K && scored;
+        a[q] = __builtin_amdgcn_raw_buffer_load_b128(ra, in ? oa + e * 2 : kOutside, 0, 0);
+        w[q] = __builtin_amdgcn_raw_buffer_load_b128(rw, in ? ow + e * 2 : kOutside, 0, 0);
+      }
+#pragma unroll
+      for (int q = 0; q < kSteps; ++q)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[q]), __builtin_bit_cast(bf16x8, a[q]), acc, 0,
+                                                      0, 0);
+    }
+    const float d = (fr & 3) == 0 ? acc[0] : (fr & 3) == 1 ? acc[1] : (fr & 3) == 2 ? acc[2] : acc[3];
+    x = __shfl(d, fr + 16 * (fr >> 2));
+  }
   if (fc != 0 || !here) return;
   const RowScore q = row_score(s);
   const float nan = __int_as_float(0x7FC00000);
@@ -159,6 +224,7 @@ auto with_shape(int M, int N, F f) {
   return f(t32);
 }
 
+// four statistics of each row and column tile
 int64_t workspace(int M, int N) {
   return with_shape(M, N, [&](auto c) { return (int64_t)((N + decltype(c)::BN - 1) / decltype(c)::BN) * 4 * M; });
 }
@@ -212,20 +278,22 @@ extern "C" int joint_logprobs(const uint16_t *A, const uint16_t *W, const float 
   if (logp && !tokens) return set_error(FUSION_E_ARG, "log probabilities of NULL tokens");
   if (!logp && !entropy && !lse) return set_error(FUSION_E_ARG, "no output buffer");
   if (workspace_floats < workspace((int)M, V)) return set_error(FUSION_E_ARG, "workspace too small");
+  if (!logp) tokens = nullptr;
   const int nct = with_shape((int)M, V, [&](auto c) -> int {
     using C = decltype(c);
     const int cols = (V + C::BN - 1) / C::BN, rows = ((int)M + C::BM - 1) / C::BM;
     if ((int64_t)cols * rows >= (1 << 23)) return -1;  // a launch holds fewer than 2^32 lanes
     const int map = tile_map(rows, cols, tiles(t128, (int)M, V) > kCus, (int)M, V, (int64_t)V * K * 2);
-    hipLaunchKernelGGL((joint_stat_kernel<C>), dim3(cols * rows), dim3(64 * C::waves), 0, stream, A, W, bias, (int)M, V,
-                       K, cols, map, workspace_);
+    const StatArgs q{A, W, bias, workspace_, (int)M, V, K, cols, map};
+    hipLaunchKernelGGL((joint_stat_kernel<C>), dim3(cols * rows), dim3(64 * C::waves), 0, stream, q);
     return cols;
   });
   if (nct < 0) return set_error(FUSION_E_UNSUPPORTED, "too many tiles: split the call along T");
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_error(e, "joint statistics launch");
-  const JoinArgs p{A, W, bias, workspace_, logp ? tokens : nullptr, parents, logp, entropy, lse, (int32_t)M, V, K, B, nct};
-  hipLaunchKernelGGL(joint_join_kernel, dim3((unsigned)((M + 63) / 64)), dim3(256), 0, stream, p);
+  const JoinArgs p{A, W, bias, workspace_, tokens, parents, logp, entropy, lse, (int32_t)M, V, K, B, nct};
+  if (M >= 64 * kCus) hipLaunchKernelGGL(joint_join_kernel<1>, dim3((unsigned)((M + 63) / 64)), dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL(joint_join_kernel<4>, dim3((unsigned)((M + 15) / 16)), dim3(256), 0, stream, p);
   e = hipGetLastError();
   return e == hipSuccess ? FUSION_OK : hip_error(e, "joint scoring launch");
 }

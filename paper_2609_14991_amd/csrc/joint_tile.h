@@ -5,13 +5,14 @@
 //
 // Tiling for gfx950: a workgroup of WM x WN waves computes a (16 TM WM) x
 // (16 TN WN) output tile, each wave (16 TM) x (16 TN) as a TM x TN grid of
-// 16 x 16 MFMA tiles.  K advances in stages of 128 bytes a row, NB of them in
+// 16 x 16 MFMA tiles.  K advances in stages of 128 (or 64) bytes a row, NB of them in
 // LDS; the operands go straight from global memory to LDS (16 bytes a lane, no
 // registers, no LDS store instructions), NB - 1 stages ahead, with one barrier
 // a stage that waits for the oldest stage's loads only.  A stage's rows are 128
 // bytes, all LDS banks, so a fragment read (16 rows, one 16-byte chunk of each)
 // would hit the same banks in every row: chunk c of row r is kept in slot
-// c ^ (r % 8), which the loading lane arranges by the global chunk it picks.
+// c ^ (r % 8), which the loading lane arranges by the global chunk it picks
+// (rows of 64 bytes: c ^ (r / 4 % 4)).
 // SQ_LDS_BANK_CONFLICT reads 0 (rows padded by 16 bytes: 47 % of the LDS's
 // active cycles).  The MFMA operands are swapped (W rows as the tile's rows),
 // so a lane ends with 4 consecutive columns of one output row.
@@ -28,7 +29,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStageBytes = 128;              // of a row
 constexpr int kMapNone = 0, kMap4x2 = 1, kMapRuns = 2;  // tiles to XCDs
 constexpr uint32_t kOutside = 0x80000000u;    // an offset past every descriptor (operands are under 2 GiB)
 
@@ -46,14 +46,16 @@ __device__ __forceinline__ void wait_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// a launch shape: WM x WN waves of TM x TN tiles, NB stages
-template <int WM_, int WN_, int TM_, int TN_, int NB_>
+// a launch shape: WM x WN waves of TM x TN tiles, NB stages of SB bytes a row
+template <int WM_, int WN_, int TM_, int TN_, int NB_, int SB_ = 128>
 struct TileShape {
-  static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NB = NB_;
+  static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NB = NB_, SB = SB_;
   static constexpr int RM = 16 * TM_, RN = 16 * TN_;  // rows and columns of a wave's tile
   static constexpr int BM = RM * WM_, BN = RN * WN_, waves = WM_ * WN_;
-  static constexpr int stage = (BM + BN) * kStageBytes;
+  static constexpr int stage = (BM + BN) * SB;
   static constexpr int lds = NB_ * stage;
+  // slot in LDS of a row's 16-byte chunk: 16 rows of one chunk meet all banks
+  static __device__ __forceinline__ int slot(int row, int chunk) { return chunk ^ (SB == 128 ? row & 7 : row >> 2 & 3); }
 };
 
 // Tile of this workgroup, which runs on XCD x = blockIdx % 8 under the hardware's
@@ -104,51 +106,93 @@ struct Bf16Op {
   }
 };
 
-// acc of the tile at row bm, column bn; row_bytes: of a row of A and W (a multiple of 16)
-template <class S, class Op>
-__device__ __forceinline__ void tile_product(Op &op, unsigned char *smem, const void *A, const void *W, int M, int N,
-                                             int row_bytes, int bm, int bn, f32x4 (&acc)[S::TM][S::TN]) {
-  constexpr int kChunks = kStageBytes / 16;      // 16-byte chunks per row and stage
-  constexpr int kRowsPer = 64 / kChunks;         // rows one wave-wide load brings (1 KiB)
-  constexpr int kLA = S::BM / kRowsPer / S::waves, kLW = S::BN / kRowsPer / S::waves, kL = kLA + kLW;  // loads per wave
-  static_assert(kLA * kRowsPer * S::waves == S::BM && kLW * kRowsPer * S::waves == S::BN, "whole loads per wave");
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = (wave / S::WN) * S::RM, wn = (wave % S::WN) * S::RN;
-
-  // Load j of a stage brings rows (j * waves + wave) * kRowsPer .. of A (j < kLA)
-  // or W to consecutive LDS: lane l lands 16 l bytes in, i.e. row l / 8, slot
-  // l % 8, and fetches the chunk which that slot holds.  Rows past the operand
-  // and, in a ragged last stage, chunks past K read as zeros (range check).
-  const __amdgpu_buffer_rsrc_t ra = rsrc(A, (uint32_t)((int64_t)M * row_bytes));
-  const __amdgpu_buffer_rsrc_t rw = rsrc(W, (uint32_t)((int64_t)N * row_bytes));
-  const int lr = lane / kChunks, lc = (lane % kChunks) ^ (lr & 7);  // kRowsPer is 8: the row's low bits are lr
-  uint32_t vo[kL];
-#pragma unroll
-  for (int j = 0; j < kL; ++j) {
-    const int row = (j < kLA ? bm + (j * S::waves + wave) * kRowsPer : bn + ((j - kLA) * S::waves + wave) * kRowsPer) + lr;
-    vo[j] = row < (j < kLA ? M : N) ? (uint32_t)((int64_t)row * row_bytes + lc * 16) : kOutside;
-  }
-  auto issue = [&](int s, int buf) {
-    unsigned char *base = smem + buf * S::stage + wave * 1024;
-    const bool ragged = (s + 1) * kStageBytes > row_bytes && s * kStageBytes + lc * 16 >= row_bytes;
-#pragma unroll
-    for (int j = 0; j < kL; ++j)
-      load_lds(j < kLA ? ra : rw, base + j * S::waves * 1024, ragged ? kOutside : vo[j], s * kStageBytes);
-  };
-
+template <class S>
+__device__ __forceinline__ void tile_zero(f32x4 (&acc)[S::TM][S::TN]) {
 #pragma unroll
   for (int i = 0; i < S::TM; ++i)
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+}
 
-  const int nk = (row_bytes + kStageBytes - 1) / kStageBytes;
-  // fragment of a 16-row operand tile: lane l holds row l % 16, the chunk of its group l / 16
-  const int fr = lane & 15, fc = lane >> 4;
-  op.begin(M, N, bm + wm + fr, bn + wn + fr, fc);
+// The loads of a tile's stages into LDS.  row_bytes: of a row of A and W (a multiple of 16)
+template <class S>
+struct TileLoads {
+  static constexpr int kChunks = S::SB / 16;      // 16-byte chunks per row and stage
+  static constexpr int kRowsPer = 64 / kChunks;   // rows one wave-wide load brings (1 KiB)
+  static constexpr int kLA = S::BM / kRowsPer / S::waves, kLW = S::BN / kRowsPer / S::waves, kL = kLA + kLW;  // loads per wave
+  static_assert(kLA * kRowsPer * S::waves == S::BM && kLW * kRowsPer * S::waves == S::BN, "whole loads per wave");
+  __amdgpu_buffer_rsrc_t ra, rw;
+  int M, N, row_bytes, wave, lr, lc;
+  uint32_t vo[kL];
+
+  __device__ __forceinline__ TileLoads(const void *A, const void *W, int M_, int N_, int row_bytes_)
+      : M(M_), N(N_), row_bytes(row_bytes_) {
+    const int lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    ra = rsrc(A, (uint32_t)((int64_t)M * row_bytes));
+    rw = rsrc(W, (uint32_t)((int64_t)N * row_bytes));
+    lr = lane / kChunks;
+    lc = S::slot(lr, lane % kChunks);  // (kRowsPer is 8 or 16: the slot goes by lr)
+  }
+  // Load j of a stage brings rows (j * waves + wave) * kRowsPer .. of A (j < kLA)
+  // or W to consecutive LDS: lane l lands 16 l bytes in, i.e. row l / kChunks, slot
+  // l % kChunks, and fetches the chunk which that slot holds.  Rows past the operand
+  // and, in a ragged last stage, chunks past K read as zeros (range check).
+  __device__ __forceinline__ void tile(int bm, int bn) {
+#pragma unroll
+    for (int j = 0; j < kL; ++j) {
+      const int row = (j < kLA ? bm + (j * S::waves + wave) * kRowsPer : bn + ((j - kLA) * S::waves + wave) * kRowsPer) + lr;
+      vo[j] = row < (j < kLA ? M : N) ? (uint32_t)((int64_t)row * row_bytes + lc * 16) : kOutside;
+    }
+  }
+  // stage s into the LDS of stage buffer `at`
+  __device__ __forceinline__ void issue(int s, unsigned char *at) const {
+    unsigned char *base = at + wave * 1024;
+    const bool ragged = (s + 1) * S::SB > row_bytes && s * S::SB + lc * 16 >= row_bytes;
+#pragma unroll
+    for (int j = 0; j < kL; ++j)
+      load_lds(j < kLA ? ra : rw, base + j * S::waves * 1024, ragged ? kOutside : vo[j], s * S::SB);
+  }
+};
+
+// adds a stage in LDS to acc, for the wave whose tile is at row wm, column wn of the
+// workgroup's.  Fragment of a 16-row operand tile: lane l holds row l % 16, the
+// chunk of its group l / 16
+template <class S, class Op>
+__device__ __forceinline__ void tile_stage(const Op &op, const unsigned char *pa, int wm, int wn, f32x4 (&acc)[S::TM][S::TN]) {
+  const int fr = threadIdx.x & 15, fc = (threadIdx.x & 63) >> 4;
+  const unsigned char *pw = pa + S::BM * S::SB;
+  auto step = [&](auto ks_) {
+    constexpr int ks = decltype(ks_)::value;
+    i32x4 fa[S::TM], fw[S::TN];
+    const int at = S::slot(fr, op.chunk(ks, fc)) * 16;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) fw[j] = *reinterpret_cast<const i32x4 *>(pw + (wn + j * 16 + fr) * S::SB + at);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) fa[i] = *reinterpret_cast<const i32x4 *>(pa + (wm + i * 16 + fr) * S::SB + at);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) acc[i][j] = op.template mfma<ks>(fw[j], fa[i], acc[i][j], j, i);
+  };
+  step(std::integral_constant<int, 0>{});
+  if constexpr (S::SB == 128) step(std::integral_constant<int, 1>{});
+}
+
+// adds the tile at row bm, column bn to acc
+template <class S, class Op>
+__device__ __forceinline__ void tile_product(Op &op, unsigned char *smem, const void *A, const void *W, int M, int N,
+                                             int row_bytes, int bm, int bn, f32x4 (&acc)[S::TM][S::TN]) {
+  TileLoads<S> loads(A, W, M, N, row_bytes);
+  constexpr int kL = TileLoads<S>::kL;
+  const int lane = threadIdx.x & 63, wave = loads.wave;
+  const int wm = (wave / S::WN) * S::RM, wn = (wave % S::WN) * S::RN;
+  loads.tile(bm, bn);
+  const int nk = (row_bytes + S::SB - 1) / S::SB;
+  op.begin(M, N, bm + wm + (lane & 15), bn + wn + (lane & 15), lane >> 4);
 #pragma unroll
   for (int s = 0; s < S::NB - 1; ++s)
-    if (s < nk) issue(s, s);
+    if (s < nk) loads.issue(s, smem + s * S::stage);
   int buf = 0;
   for (int s = 0; s < nk; ++s) {
     // stage s has landed for every wave, and every wave is done reading the
@@ -156,25 +200,8 @@ __device__ __forceinline__ void tile_product(Op &op, unsigned char *smem, const 
     if (s + S::NB - 2 < nk) wait_barrier<(S::NB - 2) * kL>();
     else wait_barrier<0>();
     op.stage(s);
-    if (s + S::NB - 1 < nk) issue(s + S::NB - 1, buf == 0 ? S::NB - 1 : buf - 1);
-    const unsigned char *pa = smem + buf * S::stage, *pw = pa + S::BM * kStageBytes;
-    auto step = [&](auto ks_) {
-      constexpr int ks = decltype(ks_)::value;
-      i32x4 fa[S::TM], fw[S::TN];
-      const int at = (op.chunk(ks, fc) ^ (fr & 7)) * 16;
-#pragma unroll
-      for (int j = 0; j < S::TN; ++j)
-        fw[j] = *reinterpret_cast<const i32x4 *>(pw + (wn + j * 16 + fr) * kStageBytes + at);
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i)
-        fa[i] = *reinterpret_cast<const i32x4 *>(pa + (wm + i * 16 + fr) * kStageBytes + at);
-#pragma unroll
-      for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-        for (int j = 0; j < S::TN; ++j) acc[i][j] = op.template mfma<ks>(fw[j], fa[i], acc[i][j], j, i);
-    };
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
+    if (s + S::NB - 1 < nk) loads.issue(s + S::NB - 1, smem + (buf == 0 ? S::NB - 1 : buf - 1) * S::stage);
+    tile_stage<S>(op, smem + buf * S::stage, wm, wn, acc);
     buf = buf == S::NB - 1 ? 0 : buf + 1;
   }
 }

@@ -152,6 +152,7 @@ __global__ void __launch_bounds__(64 * S::waves, 2) mx_proj_kernel(MxArgs p) {
   int tr, tc;
   tile_place(p.map, p.n_col_tiles, tr, tc);
   f32x4 acc[S::TM][S::TN];
+  tile_zero<S>(acc);
   MxOp<S::TM, S::TN> op;
   op.A_scales = p.A_scales;
   op.W_scales = p.W_scales;

@@ -9,7 +9,7 @@
 
 namespace fusion {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // stands for -infinity in x - max: e^it is 0, and 0 times it is 0 and not NaN
 constexpr float kFar = -1e4f;
 
@@ -42,6 +42,16 @@ __device__ __forceinline__ float wave_add(float x) {
 }
 __device__ __forceinline__ int wave_min(int x) {
   return wave_reduce(INT_MAX, x, [](int a, int b) { return min(a, b); });
+}
+
+// op over lanes l, l ^ 16, l ^ 32 and l ^ 48, the result in all four: exchanging a
+// register with itself leaves the two sides' values in its two copies
+template <class F>
+__device__ __forceinline__ float across_rows(float x, F op) {
+  auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = op(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return op(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
@@ -99,6 +109,13 @@ __device__ __forceinline__ void stat_wave(Stat &s) {
   s.ones = wave_add(s.ones);
   s.rest = wave_add(s.rest);
   s.u = wave_add(s.u);
+}
+
+// those of lanes l, l ^ 16, l ^ 32 and l ^ 48 as one, in all four
+__device__ __forceinline__ Stat stat_across(Stat s) {
+  const auto add = [](float a, float b) { return a + b; };
+  stat_lift(s, across_rows(s.m, [](float a, float b) { return fmaxf(a, b); }));
+  return Stat{s.m, across_rows(s.ones, add), across_rows(s.rest, add), across_rows(s.u, add)};
 }
 
 // what a finished set's statistics say
