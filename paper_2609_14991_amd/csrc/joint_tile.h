@@ -5,14 +5,13 @@
 //
 // Tiling for gfx950: a workgroup of WM x WN waves computes a (16 TM WM) x
 // (16 TN WN) output tile, each wave (16 TM) x (16 TN) as a TM x TN grid of
-// 16 x 16 MFMA tiles.  K advances in stages of 128 (or 64) bytes a row, NB of them in
+// 16 x 16 MFMA tiles.  K advances in stages of 128 bytes a row, NB of them in
 // LDS; the operands go straight from global memory to LDS (16 bytes a lane, no
 // registers, no LDS store instructions), NB - 1 stages ahead, with one barrier
 // a stage that waits for the oldest stage's loads only.  A stage's rows are 128
 // bytes, all LDS banks, so a fragment read (16 rows, one 16-byte chunk of each)
 // would hit the same banks in every row: chunk c of row r is kept in slot
 // c ^ (r % 8), which the loading lane arranges by the global chunk it picks
-// (rows of 64 bytes: c ^ (r / 4 % 4)).
 // SQ_LDS_BANK_CONFLICT reads 0 (rows padded by 16 bytes: 47 % of the LDS's
 // active cycles).  The MFMA operands are swapped (W rows as the tile's rows),
 // so a lane ends with 4 consecutive columns of one output row.
@@ -35,6 +34,14 @@ constexpr uint32_t kOutside = 0x80000000u;    // an offset past every descriptor
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void *base, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), (short)0, (int)bytes, 0x00020000);
 }
+// the same of values that are uniform without the compiler seeing it, which would
+// otherwise go through the lanes' descriptors one by one at each access
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_uniform(const void *base, uint32_t bytes) {
+  const uint64_t v = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+  return rsrc(reinterpret_cast<const void *>((uint64_t)hi << 32 | lo), (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes));
+}
 // 16 bytes per lane straight into LDS (lane l lands at lds + 16 l)
 __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, unsigned char *lds, uint32_t voff, uint32_t soff) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)lds, 16, voff, soff, 0, 0);
@@ -46,16 +53,25 @@ __device__ __forceinline__ void wait_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// a launch shape: WM x WN waves of TM x TN tiles, NB stages of SB bytes a row
-template <int WM_, int WN_, int TM_, int TN_, int NB_, int SB_ = 128>
+// Slot in LDS of a 16-byte chunk of a row, rows of 128 or 64 bytes: 16 rows' reads
+// of one chunk meet all banks
+struct Slots128 {
+  static __device__ __forceinline__ int of(int row, int chunk) { return chunk ^ (row & 7); }
+};
+struct Slots64 {
+  static __device__ __forceinline__ int of(int row, int chunk) { return chunk ^ (row >> 2 & 3); }
+};
+
+// a launch shape: WM x WN waves of TM x TN tiles, NB stages
+template <int WM_, int WN_, int TM_, int TN_, int NB_ = 1>
 struct TileShape {
-  static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NB = NB_, SB = SB_;
+  static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, NB = NB_;
+  static constexpr int SB = 128;  // bytes of a row in a stage
   static constexpr int RM = 16 * TM_, RN = 16 * TN_;  // rows and columns of a wave's tile
   static constexpr int BM = RM * WM_, BN = RN * WN_, waves = WM_ * WN_;
   static constexpr int stage = (BM + BN) * SB;
   static constexpr int lds = NB_ * stage;
-  // slot in LDS of a row's 16-byte chunk: 16 rows of one chunk meet all banks
-  static __device__ __forceinline__ int slot(int row, int chunk) { return chunk ^ (SB == 128 ? row & 7 : row >> 2 & 3); }
+  static constexpr int seg = RN < 64 ? RN : 64;  // columns of a stored row segment
 };
 
 // Tile of this workgroup, which runs on XCD x = blockIdx % 8 under the hardware's
@@ -132,7 +148,7 @@ struct TileLoads {
     ra = rsrc(A, (uint32_t)((int64_t)M * row_bytes));
     rw = rsrc(W, (uint32_t)((int64_t)N * row_bytes));
     lr = lane / kChunks;
-    lc = S::slot(lr, lane % kChunks);  // (kRowsPer is 8 or 16: the slot goes by lr)
+    lc = Slots128::of(lr, lane % kChunks);  // (kRowsPer is 8: the row's low bits are lr)
   }
   // Load j of a stage brings rows (j * waves + wave) * kRowsPer .. of A (j < kLA)
   // or W to consecutive LDS: lane l lands 16 l bytes in, i.e. row l / kChunks, slot
@@ -165,7 +181,7 @@ __device__ __forceinline__ void tile_stage(const Op &op, const unsigned char *pa
   auto step = [&](auto ks_) {
     constexpr int ks = decltype(ks_)::value;
     i32x4 fa[S::TM], fw[S::TN];
-    const int at = S::slot(fr, op.chunk(ks, fc)) * 16;
+    const int at = Slots128::of(fr, op.chunk(ks, fc)) * 16;
 #pragma unroll
     for (int j = 0; j < S::TN; ++j) fw[j] = *reinterpret_cast<const i32x4 *>(pw + (wn + j * 16 + fr) * S::SB + at);
 #pragma unroll
@@ -176,7 +192,7 @@ __device__ __forceinline__ void tile_stage(const Op &op, const unsigned char *pa
       for (int j = 0; j < S::TN; ++j) acc[i][j] = op.template mfma<ks>(fw[j], fa[i], acc[i][j], j, i);
   };
   step(std::integral_constant<int, 0>{});
-  if constexpr (S::SB == 128) step(std::integral_constant<int, 1>{});
+  step(std::integral_constant<int, 1>{});
 }
 
 // adds the tile at row bm, column bn to acc
@@ -206,32 +222,17 @@ __device__ __forceinline__ void tile_product(Op &op, unsigned char *smem, const 
   }
 }
 
-// Stores a tile with its bias.  In the accumulator of a 16 x 16 tile lane l holds
-// output row l % 16, columns 4 * (l / 16) .. + 3.  Each 16-row slab of the wave's
-// tile goes through the wave's own LDS area (free once every wave has read the last
-// stage), chunks swizzled by the row as above, and leaves as whole row segments
-// of kSeg columns, kRowsI rows a store.  The bias is fetched before the first
-// store: a load behind stores would wait for all of them.
+// Stores a wave's tile, at row m0, column n0 of the output.  In the accumulator of
+// a 16 x 16 tile lane l holds output row l % 16, columns 4 * (l / 16) .. + 3.  Each
+// 16-row slab of the tile goes through the wave's own LDS area, chunks swizzled by
+// the row as above, and leaves as whole row segments of S::seg columns, kRowsI rows
+// a store, with the bias bv of the lane's columns of each segment added.
 // kAux: cache policy of the output stores (see joint_project)
 template <class S, int kAux>
-__device__ __forceinline__ void tile_store(unsigned char *smem, const float *__restrict__ bias, int M, int N, int bm,
-                                           int bn, const f32x4 (&acc)[S::TM][S::TN], float *__restrict__ out) {
-  constexpr int kSeg = S::RN < 64 ? S::RN : 64, kLanes = kSeg / 4, kRowsI = 64 / kLanes;
-  static_assert(S::lds >= S::waves * 16 * kSeg * 4, "LDS too small for the epilogue");
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = (wave / S::WN) * S::RM, wn = (wave % S::WN) * S::RN;
-  const int fr = lane & 15, fc = lane >> 4;
-  float bv[S::RN / kSeg][4];
-#pragma unroll
-  for (int sg = 0; sg < S::RN / kSeg; ++sg)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = bn + wn + sg * kSeg + (lane % kLanes) * 4 + r;
-      bv[sg][r] = (bias && n < N) ? bias[n] : 0.0f;
-    }
-  wait_barrier<0>();
-  f32x4 *slab = reinterpret_cast<f32x4 *>(smem) + wave * 16 * kLanes;
+__device__ __forceinline__ void slab_store(f32x4 *slab, const float (&bv)[S::RN / S::seg][4], int M, int N, int m0_, int n0,
+                                           const f32x4 (&acc)[S::TM][S::TN], float *__restrict__ out) {
+  constexpr int kSeg = S::seg, kLanes = kSeg / 4, kRowsI = 64 / kLanes;
+  const int lane = threadIdx.x & 63, fr = lane & 15, fc = lane >> 4;
   const int orow = lane / kLanes, ochunk = lane % kLanes;
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
@@ -241,7 +242,7 @@ __device__ __forceinline__ void tile_store(unsigned char *smem, const float *__r
       for (int j = 0; j < kSeg / 16; ++j)
         slab[fr * kLanes + ((j * 4 + fc) ^ (fr & (kLanes - 1)))] = acc[i][sg * (kSeg / 16) + j];
       __builtin_amdgcn_wave_barrier();
-      const int n = bn + wn + sg * kSeg + ochunk * 4;
+      const int n = n0 + sg * kSeg + ochunk * 4;
 #pragma unroll
       for (int q = 0; q < 16 / kRowsI; ++q) {
         const int row = q * kRowsI + orow;
@@ -250,9 +251,9 @@ __device__ __forceinline__ void tile_store(unsigned char *smem, const float *__r
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[r] = __float_as_int(x[r] + bv[sg][r]);
         // a descriptor of this store's rows that exist; columns past N fall outside it
-        const int m0 = bm + wm + i * 16 + q * kRowsI;
+        const int m0 = m0_ + i * 16 + q * kRowsI;
         const int rows = min(max(M - m0, 0), kRowsI);
-        const __amdgpu_buffer_rsrc_t ro = rsrc(out + (int64_t)m0 * N, (uint32_t)rows * (uint32_t)N * 4u);
+        const __amdgpu_buffer_rsrc_t ro = rsrc_uniform(out + (int64_t)m0 * N, (uint32_t)rows * (uint32_t)N * 4u);
         const uint32_t o = ((uint32_t)orow * (uint32_t)N + (uint32_t)n) * 4u;
         __builtin_amdgcn_raw_buffer_store_b128(v, ro, n + 3 < N ? o : kOutside, 0, kAux);
         if (N % 4 != 0) {  // uniform: the row's last columns, one at a time
@@ -264,6 +265,29 @@ __device__ __forceinline__ void tile_store(unsigned char *smem, const float *__r
       __builtin_amdgcn_wave_barrier();
     }
   }
+}
+
+// Stores the workgroup's tile: the slabs are the stages' LDS, free once every wave
+// has read the last stage.  The bias is fetched before the first store: a load
+// behind stores would wait for all of them.
+template <class S, int kAux>
+__device__ __forceinline__ void tile_store(unsigned char *smem, const float *__restrict__ bias, int M, int N, int bm,
+                                           int bn, const f32x4 (&acc)[S::TM][S::TN], float *__restrict__ out) {
+  constexpr int kSeg = S::seg, kLanes = kSeg / 4;
+  static_assert(S::lds >= S::waves * 16 * kSeg * 4, "LDS too small for the epilogue");
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = (wave / S::WN) * S::RM, wn = (wave % S::WN) * S::RN;
+  float bv[S::RN / kSeg][4];
+#pragma unroll
+  for (int sg = 0; sg < S::RN / kSeg; ++sg)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int n = bn + wn + sg * kSeg + (lane % kLanes) * 4 + r;
+      bv[sg][r] = (bias && n < N) ? bias[n] : 0.0f;
+    }
+  wait_barrier<0>();
+  slab_store<S, kAux>(reinterpret_cast<f32x4 *>(smem) + wave * 16 * kLanes, bv, M, N, bm + wm, bn + wn, acc, out);
 }
 
 }  // namespace fusion

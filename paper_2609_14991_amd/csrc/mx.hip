@@ -8,8 +8,10 @@
 // nearest level, halfway to the even code, above 6 to 6.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <type_traits>
+#include <utility>
 
 #include "fusion_internal.h"
 #include "joint_tile.h"
@@ -93,6 +95,15 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t *__restri
   __builtin_memcpy(out + row * stride + col, &p, 16);
 }
 
+// 16 x 16 outputs over 128 of K, both operands fp4: lane l holds row l % 16's block
+// l / 16 of each, and that block's scale in byte bw or ba of its register
+template <int bw, int ba>
+__device__ __forceinline__ f32x4 mfma_mx(i32x4 w, i32x4 a, f32x4 c, int sw, int sa) {
+  const i32x8 w8 = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
+  const i32x8 a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, bw, sw, ba, sa);
+}
+
 // Operands of the product: a stage is 256 elements of K, 8 blocks a row, two steps
 // of v_mfma_scale_f32_16x16x128_f8f6f4.  A lane of group g reads chunks (blocks) 2 g
 // and 2 g + 1, one a step: any split of K over the groups gives the same sum, and
@@ -133,9 +144,7 @@ struct MxOp {
   static __device__ __forceinline__ int chunk(int ks, int fc) { return 2 * fc + ks; }
   template <int ks>
   __device__ __forceinline__ f32x4 mfma(i32x4 w, i32x4 a, f32x4 c, int j, int i) const {
-    const i32x8 w8 = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
-    const i32x8 a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8, a8, c, 4, 4, ks, sw[j], ks, sa[i]);
+    return mfma_mx<ks, ks>(w, a, c, sw[j], sa[i]);
   }
 };
 
@@ -160,6 +169,153 @@ __global__ void __launch_bounds__(64 * S::waves, 2) mx_proj_kernel(MxArgs p) {
   op.stride = FUSION_MX_SCALE_STRIDE(p.K);
   tile_product<S>(op, smem, p.A, p.W, p.M, p.N, p.K / 2, tr * S::BM, tc * S::BN, acc);
   tile_store<S, kAux>(smem, p.bias, p.M, p.N, tr * S::BM, tc * S::BN, acc, p.out);
+}
+
+// The same product for launches that the output's stores bound.  Two things keep
+// stores and products from overlapping in a tile kernel: a wave's loads and stores
+// complete in one order, so that a wave which stores a tile and then waits for the
+// next one's operands waits for its stores; and operands of 4 bits are used up so
+// fast that bringing both takes longer than their product.  Here a workgroup keeps
+// its 128 columns of W in registers, all of K, and goes down the rows of A, 64 at a
+// time; two waves do all the loading, a tile each in turn, and the four that multiply
+// and store wait for nothing but their barrier.  Two workgroups a CU, out of step.
+// 64 rows x 128 columns, 32 x 64 a wave: it stores 256 bytes of a row at once (204 us
+// for 76800 x 4096 x 640, 230 in 128 bytes).  From 6 steps of 128 along K on, W's
+// registers allow 32 columns a wave only.
+template <int steps>
+using Panel = std::conditional_t<steps <= 5, TileShape<2, 2, 2, 4>, TileShape<1, 4, 4, 2>>;
+constexpr int kPanelSteps = 6, kPanelRows = 64, kPanelCols = 128;
+
+struct PanelArgs {
+  MxArgs g;
+  int slices, row_tiles;  // a workgroup takes a column tile and every slices-th row tile
+};
+
+template <class F, int... s>
+__device__ __forceinline__ void each_step(F f, std::integer_sequence<int, s...>) {
+  (f(std::integral_constant<int, s>{}), ...);
+}
+
+// steps: of 128 along K, each unrolled
+template <int steps, int kAux>
+__global__ void __launch_bounds__(64 * 6, 3) mx_panel_kernel(PanelArgs q) {
+  typedef Panel<steps> S;
+  static_assert(S::BM == kPanelRows && S::BN == kPanelCols, "as the launch takes them");
+  const MxArgs &p = q.g;
+  // a buffer: a tile of A, steps x 64 rows x 64 bytes, then its scales' rows
+  constexpr int kScales = steps * S::BM * 64, kBuf = kScales + S::BM * FUSION_MX_SCALE_STRIDE(128 * steps);
+  __shared__ __align__(1024) unsigned char s_buf[2][kBuf];
+  __shared__ f32x4 s_slab[S::waves][4 * S::seg];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int fr = lane & 15, fc = lane >> 4;
+  constexpr int stride = FUSION_MX_SCALE_STRIDE(128 * steps);  // (of K too: it goes by whole 256s)
+  const int blocks = p.K / kBlock;
+  // a run of consecutive workgroups, column-fastest, on each XCD: its L2 fetches a
+  // slice's rows of A once, and merges the lines that neighbouring columns share
+  const int x = blockIdx.x & 7, per = gridDim.x >> 3, more = gridDim.x & 7;
+  const int unit = x * per + min(x, more) + (blockIdx.x >> 3);
+  const int slice = __builtin_amdgcn_readfirstlane(unit / p.n_col_tiles), col = unit - slice * p.n_col_tiles;
+  const int tiles = __builtin_amdgcn_readfirstlane((q.row_tiles - slice + q.slices - 1) / q.slices);
+
+  if (wave >= S::waves) {
+    const int who = wave - S::waves;
+    const __amdgpu_buffer_rsrc_t ra = rsrc(p.A, (uint32_t)((int64_t)p.M * (p.K / 2)));
+    const __amdgpu_buffer_rsrc_t rs = rsrc(p.A_scales, (uint32_t)((int64_t)p.M * stride));
+    // a load brings 16 rows of a step, 4 chunks each; lane l's lands in row l / 4, slot l % 4
+    const int row = lane >> 2, chunk = Slots64::of(row, lane & 3);
+    auto issue = [&](int k) {
+      const int tile = slice + k * q.slices;
+      unsigned char *at = s_buf[who];
+      uint32_t vo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = tile * S::BM + j * 16 + row;
+        vo[j] = r < p.M ? (uint32_t)(r * (int64_t)(p.K / 2) + chunk * 16) : kOutside;
+      }
+#pragma unroll
+      for (int s = 0; s < steps; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          load_lds(ra, at + (s * 4 + j) * 1024, s < steps - 1 || s * 4 + chunk < blocks ? vo[j] : kOutside, s * 64);
+      // the scales of 64 rows lie together: 256 bytes a load (past the operand: zeros)
+      const uint32_t so = (uint32_t)((int64_t)tile * S::BM * stride + lane * 4);
+#pragma unroll
+      for (int j = 0; j < stride / 4; ++j)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(at + kScales + j * 256), 4, so,
+                                                 j * 256, 0, 0);
+    };
+    // the workgroup's tiles `who`, `who` + 2 ..: each into this wave's buffer, once
+    // the others are behind the barrier of the tile after the one that was there
+    if (who == 0) issue(0);
+    for (int k = 0; k < tiles; ++k) {
+      if (k % 2 == who) wait_barrier<0>();
+      else {
+        asm volatile("s_barrier" ::: "memory");
+        if (k + 1 < tiles) issue(k + 1);
+      }
+    }
+    return;
+  }
+
+  const int bn = col * S::BN + wave % S::WN * S::RN, wm = wave / S::WN * S::RM;
+  i32x4 w[steps][S::TN];
+  int sw[(steps + 3) / 4][S::TN] = {};  // a byte a step
+  const __amdgpu_buffer_rsrc_t rw = rsrc(p.W, (uint32_t)((int64_t)p.N * (p.K / 2)));
+  const __amdgpu_buffer_rsrc_t rv = rsrc(p.W_scales, (uint32_t)((int64_t)p.N * stride));
+#pragma unroll
+  for (int s = 0; s < steps; ++s)
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int n = bn + j * 16 + fr, c = s * 4 + fc;
+      const bool in = n < p.N && c < blocks;
+      w[s][j] = __builtin_amdgcn_raw_buffer_load_b128(rw, in ? (uint32_t)(n * (int64_t)(p.K / 2) + c * 16) : kOutside, 0, 0);
+      sw[s / 4][j] |= (int)__builtin_amdgcn_raw_buffer_load_b8(rv, in ? (uint32_t)(n * (int64_t)stride + c) : kOutside, 0, 0) << (s % 4 * 8);
+    }
+  constexpr int kLanes = S::seg / 4;
+  static_assert(S::seg == S::RN, "one segment a row");
+  float bv[1][4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int n = bn + lane % kLanes * 4 + r;
+    bv[0][r] = p.bias && n < p.N ? p.bias[n] : 0.0f;
+  }
+  for (int k = 0; k < tiles; ++k) {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const unsigned char *at = s_buf[k & 1];
+    f32x4 acc[S::TM][S::TN];
+    tile_zero<S>(acc);
+    auto step = [&](auto s_) {
+      constexpr int s = decltype(s_)::value;
+      i32x4 a[S::TM];
+      int sa[S::TM];
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) {
+        a[i] = *reinterpret_cast<const i32x4 *>(at + s * 4096 + (wm + i * 16 + fr) * 64 + Slots64::of(fr, fc) * 16);
+        sa[i] = at[kScales + (wm + i * 16 + fr) * stride + s * 4 + fc];
+      }
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) sa[i] &= s * 4 + fc < blocks ? 0xFF : 0;  // (bytes behind the last block mean nothing)
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) acc[i][j] = mfma_mx<s % 4, 0>(w[s][j], a[i], acc[i][j], sw[s / 4][j], sa[i]);
+    };
+    each_step(step, std::make_integer_sequence<int, steps>{});
+    slab_store<S, kAux>(s_slab[wave], bv, p.M, p.N, (slice + k * q.slices) * S::BM + wm, bn, acc, p.out);
+  }
+}
+
+template <int... s>
+void launch_panel(const PanelArgs &q, hipStream_t stream, std::integer_sequence<int, s...>) {
+  const dim3 grid(q.slices * q.g.n_col_tiles), block(64 * 6);
+  const int steps = (q.g.K + 127) / 128;
+  // streaming stores for rows of whole 128-byte lines, as in joint_project
+  auto go = [&](auto n) {
+    if (steps != decltype(n)::value) return;
+    if (q.g.N % 32 == 0) hipLaunchKernelGGL((mx_panel_kernel<decltype(n)::value, 18>), grid, block, 0, stream, q);
+    else hipLaunchKernelGGL((mx_panel_kernel<decltype(n)::value, 0>), grid, block, 0, stream, q);
+  };
+  (go(std::integral_constant<int, s + 1>{}), ...);
 }
 
 int check_mx(int32_t dtype, int64_t stride, int32_t R, int32_t K) {
@@ -254,6 +410,23 @@ extern "C" int joint_project_mx(const uint8_t *A, const uint8_t *A_scales, const
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? FUSION_OK : hip_error(e, "4-bit projection launch");
   };
+  // By panels from 512 tiles of 128 x 128 on and up to the K that W's registers hold
+  // (us, tiles and panels): 76800 x 4096 x 640 299 and 194, 3328 x 4096 x 640 18.9 and
+  // 15.9, 30000 x 2500 x 640 88 and 84, 97585 x 401 x 64 35 and 29; below that the two
+  // are level, and with few columns or a long K tiles ahead (1024 x 1024 x 512 4.9 and
+  // 5.9).  Not for many rows that share lines with their neighbours and a short K: the
+  // workgroups of neighbouring columns drift apart, and the L2 merges fewer of those
+  // lines (52396 x 3209 x 32 134 and 173, 145915 x 1459 x 128 186 and 226; of 12 such
+  // sizes two were better off: 26090 x 8441 x 96 269 and 218).
+  const bool drifts = N % 32 != 0 && K <= 128 && tiles(t128) >= 4500;
+  if (K <= 128 * kPanelSteps && tiles(t128) >= 512 && !drifts) {
+    PanelArgs q{{A, A_scales, W, W_scales, bias, out, M, N, K, (N + kPanelCols - 1) / kPanelCols, 0}, 1,
+                (M + kPanelRows - 1) / kPanelRows};
+    q.slices = std::max<int>(1, std::min<int>(2 * kCus / q.g.n_col_tiles, q.row_tiles));
+    launch_panel(q, stream, std::make_integer_sequence<int, kPanelSteps>{});
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? FUSION_OK : hip_error(e, "4-bit projection launch");
+  }
   // the largest tile that fills the chip
   if (tiles(t256) >= 1000 && N > 128) return go(t256);
   if (tiles(t128) > kCus) return go(t128);

@@ -253,7 +253,9 @@ def test_product(M, N, K):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("M,N,K", [(33001, 2050, 96), (32768, 2048, 640), (9000, 130, 256), (70001, 100, 64)])
+@pytest.mark.parametrize("M,N,K", [(33001, 2050, 96), (32768, 2048, 640), (9000, 130, 256), (70001, 100, 64), (40000, 1001, 32),
+                                   (33000, 1030, 1056), (130000, 130, 288), (8200, 1002, 768),
+                                   (16500, 517, 160), (50000, 2001, 96), (70000, 200, 640)])
 def test_product_of_many_rows(M, N, K):
     a = _operands(np.random.default_rng(M), M, N, K)
     rows = np.unique(np.concatenate([np.random.default_rng(1).choice(M, 150), [0, M - 1]]))
