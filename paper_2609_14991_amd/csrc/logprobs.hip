@@ -10,6 +10,7 @@
 //                                      - g_entropy p_y (log p_y + entropy)
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "fusion_internal.h"
@@ -21,9 +22,12 @@ namespace {
 
 __device__ int32_t g_score_status;
 
-constexpr int kPer = 16;          // values a lane holds of a wave's chunk
+typedef int Words __attribute__((ext_vector_type(4)));
+typedef int UnalignedWords __attribute__((ext_vector_type(4), aligned(2)));
+
+constexpr int kPer = 16;           // values a lane holds of a wave's chunk
 constexpr int kChunk = 64 * kPer;  // columns of a chunk
-constexpr int kList = 128;        // candidates a wave keeps
+constexpr int kList = 128;         // candidates a wave keeps
 
 // Column of value j of a lane's chunk
 template <class T>
@@ -47,13 +51,13 @@ __device__ __forceinline__ void load_chunk(const T *row, int V, int base, int la
   }
   Pack<T> p[kPer / n];
 #pragma unroll
-  for (int i = 0; i < kPer / n; ++i)
-    __builtin_memcpy(&p[i], row + min(base + (i * 64 + lane) * n, V - n), 16);
+  for (int i = 0; i < kPer / n; ++i) __builtin_memcpy(&p[i], row + min(base + (i * 64 + lane) * n, V - n), 16);
 #pragma unroll
   for (int j = 0; j < kPer; ++j) x[j] = to_float(p[j / n].v[j % n]);
   if (base + kChunk > V) {
 #pragma unroll
     for (int i = 0; i < kPer / n; ++i) {
+      if (base + (i + 1) * 64 * n <= V) continue;  // uniform
       const int shift = base + (i * 64 + lane) * n - (V - n);
 #pragma unroll
       for (int b = 1; b < n; b *= 2)
@@ -67,8 +71,6 @@ __device__ __forceinline__ void load_chunk(const T *row, int V, int base, int la
   }
 }
 
-__device__ __forceinline__ bool before(float va, int ia, float vb, int ib) { return va > vb || (va == vb && ia < ib); }
-
 // Orders a wave's own LDS writes before its later LDS reads by other lanes
 __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
@@ -76,45 +78,44 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
 }
 
-// The k best (value descending, id ascending) of two entries a lane (-infinity:
-// none); lane r < k ends with the r-th, and with (-infinity, -1) where there is none
-__device__ __forceinline__ void pick_best(float v0, int i0, float v1, int i1, int k, int lane, float &v, int &id) {
-  v = -INFINITY;
+// The k best (value descending, id ascending) of two entries a lane, values by
+// their order (none: kNone); lane r < k ends with the r-th, kNone where there is none
+constexpr int kNone = INT_MIN;
+__device__ __forceinline__ bool before(int va, int ia, int vb, int ib) { return va > vb || (va == vb && ia < ib); }
+__device__ __forceinline__ void pick_best(int v0, int i0, int v1, int i1, int k, int lane, int &v, int &id) {
+  v = kNone;
   id = -1;
   for (int r = 0; r < k; ++r) {
     const bool second = before(v1, i1, v0, i0);
-    const float b = second ? v1 : v0;
-    const float w = wave_max(b);
-    if (w == -INFINITY) break;
+    const int b = second ? v1 : v0;
+    const int w = wave_max(b);
+    if (w == kNone) break;
     const int bi = wave_min(b == w ? (second ? i1 : i0) : INT_MAX);
     if (lane == r) {
       v = w;
       id = bi;
     }
-    if (v0 == w && i0 == bi) v0 = -INFINITY;
-    if (v1 == w && i1 == bi) v1 = -INFINITY;
+    if (v0 == w && i0 == bi) v0 = kNone;
+    if (v1 == w && i1 == bi) v1 = kNone;
   }
 }
 
-// The candidates for the k best of the columns a wave has seen: a list in LDS,
-// of which at least k (or all there are) are no worse than (floor_v, floor_id),
-// and which holds everything that is better
+// The candidates for the k best of the columns a wave has seen: a list in LDS that
+// holds at least k (or all there are) which are no less than `floor`, and all that
+// are greater; -infinity is none
 struct Best {
-  float *val;
-  int *id;
-  int count = 0;  // uniform
-  float floor_v = -INFINITY;
-  int floor_id = -1;
+  int *val, *id;  // (order, column)
+  int count;      // uniform, as the floor
+  float floor;
 };
 
 // keeps the k best of the list, in order
 __device__ __forceinline__ void best_shrink(Best &b, int k, int lane) {
   wave_lds_sync();
   const bool h0 = lane < b.count, h1 = lane + 64 < b.count;
-  const float v0 = h0 ? b.val[lane] : -INFINITY, v1 = h1 ? b.val[lane + 64] : -INFINITY;
+  const int v0 = h0 ? b.val[lane] : kNone, v1 = h1 ? b.val[lane + 64] : kNone;
   const int i0 = h0 ? b.id[lane] : INT_MAX, i1 = h1 ? b.id[lane + 64] : INT_MAX;
-  float v;
-  int id;
+  int v, id;
   pick_best(v0, i0, v1, i1, k, lane, v, id);
   wave_lds_sync();
   b.count = min(b.count, k);
@@ -122,48 +123,75 @@ __device__ __forceinline__ void best_shrink(Best &b, int k, int lane) {
     b.val[lane] = v;
     b.id[lane] = id;
   }
-  if (b.count == k) {
-    b.floor_v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), k - 1));
-    b.floor_id = __builtin_amdgcn_readlane(id, k - 1);
-  }
+  if (b.count == k) b.floor = of_order(__builtin_amdgcn_readlane(v, k - 1));
   wave_lds_sync();
 }
 
-// the columns of one more chunk, which lie behind all seen before
+// the columns of one more chunk, which lie behind all seen before; top: of the lane's,
+// chunk_top: of the chunk's
 template <class T>
-__device__ __forceinline__ void best_take(Best &b, const float (&x)[kPer], float lane_max, int base, int k, int lane,
-                                          bool first) {
+__device__ __forceinline__ void best_take(Best &b, const float (&x)[kPer], float top, float chunk_top, int base, int k,
+                                          int lane, bool first) {
+  float above = b.floor;  // a column behind the k that are no less than the floor has to exceed it
   if (first) {
     // the k-th largest of the lanes' maxima: at least k columns are no less
-    float left = lane_max;
-    for (int r = 0; r < k; ++r) {
-      b.floor_v = wave_max(left);
-      if (b.floor_v == -INFINITY) break;
-      if (lane == __builtin_ctzll(__ballot(left == b.floor_v))) left = -INFINITY;
+    int left = order_of(top), at = order_of(chunk_top);
+    for (int r = 1; r < k; ++r) {
+      if (lane == __builtin_ctzll(__ballot(left == at))) left = kNone;
+      at = wave_max(left);
     }
-    b.floor_id = b.floor_v == -INFINITY ? -1 : INT_MAX;
-  } else {
-    b.floor_id = -1;  // a column behind the k that are no less than the floor has to exceed it
-    if (!__ballot(lane_max > b.floor_v)) return;
+    b.floor = of_order(at);
+    above = of_order(at == 0 ? -2 : at - 1);  // the float below (-1 is -0)
+    if (!(b.floor > -INFINITY)) b.floor = above = -INFINITY;  // fewer lanes than k hold any
+  } else if (!(chunk_top > above)) {
+    return;
   }
+  // (the comparisons first, then the few that hold anything: 16 comparisons with a
+  // branch each 173 -> 180 us for 76800 rows of 4096 in bf16, 4 alternatives)
+  unsigned long long mask[kPer];
+  int more = 0;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    const int c = column<T>(base, lane, j);
-    bool in = before(x[j], c, b.floor_v, b.floor_id);
-    unsigned long long mask = __ballot(in);
-    if (!mask) continue;
-    if (b.count + __popcll(mask) > kList) {
-      best_shrink(b, k, lane);
-      in = before(x[j], c, b.floor_v, b.floor_id);
-      mask = __ballot(in);
-    }
-    if (in) {
-      const int at = b.count + __builtin_amdgcn_mbcnt_hi(mask >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-      b.val[at] = x[j];
-      b.id[at] = c;
-    }
-    b.count += __popcll(mask);
+    mask[j] = __ballot(x[j] > above);
+    more += __popcll(mask[j]);
   }
+  if (b.count + more <= kList) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if (!mask[j]) continue;
+      if (x[j] > above) {
+        const int at = b.count + __builtin_amdgcn_mbcnt_hi(mask[j] >> 32, __builtin_amdgcn_mbcnt_lo((uint32_t)mask[j], 0));
+        b.val[at] = order_of(x[j]);
+        b.id[at] = column<T>(base, lane, j);
+      }
+      b.count += __popcll(mask[j]);
+    }
+    return;
+  }
+  // many candidates (long runs of equal or rising values): the k best so far, and the
+  // chunk's k best one by one, each the best behind the one before
+  if (b.count > k) best_shrink(b, k, lane);
+  int last_v = INT_MAX, last_id = -1;
+  for (int r = 0; r < k; ++r) {
+    int v = kNone, id = INT_MAX;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int o = order_of(x[j]), c = column<T>(base, lane, j);
+      if (x[j] > -INFINITY && before(last_v, last_id, o, c) && before(o, c, v, id)) {
+        v = o;
+        id = c;
+      }
+    }
+    last_v = wave_max(v);
+    if (last_v == kNone) break;
+    last_id = wave_min(v == last_v ? id : INT_MAX);
+    if (lane == 0) {
+      b.val[b.count] = last_v;
+      b.id[b.count] = last_id;
+    }
+    ++b.count;
+  }
+  best_shrink(b, k, lane);
 }
 
 struct ScoreArgs {
@@ -175,11 +203,13 @@ struct ScoreArgs {
   int32_t M, B, V, k;
 };
 
-// W waves a token: 4 tokens a workgroup of 256 lanes with one wave each, else one
+// W waves a token: 4 tokens a workgroup of 256 lanes with one wave each, else one.
+// (32 values a lane instead of 16: half the waves fit, 173 -> 204 us for 76800 rows
+// of 4096 in bf16 with 4 alternatives.)
 template <class T, int W>
 __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs p) {
   constexpr int kWaves = W == 1 ? 4 : W;
-  __shared__ float s_val[kWaves][kList];
+  __shared__ int s_val[kWaves][kList];
   __shared__ int s_id[kWaves][kList];
   __shared__ Stat s_stat[kWaves];
   __shared__ int s_count[kWaves];
@@ -194,28 +224,24 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs 
   const T *row = static_cast<const T *>(p.logits) + (dead ? 0 : r) * p.stride;
   float x_tok = 0.0f;
   if (!dead && tok >= 0 && !bad_token) x_tok = to_float(row[tok]);
-  Stat s = stat_none();
-  Best b;
-  b.val = s_val[wave];
-  b.id = s_id[wave];
+  WaveStat ws = wave_stat_none();
+  Best b{s_val[wave], s_id[wave], 0, -INFINITY};
   if (!dead) {
-    bool first = true;
-    for (int base = (W == 1 ? 0 : wave) * kChunk; base < p.V; base += W * kChunk) {
+    const int start = (W == 1 ? 0 : wave) * kChunk;
+    for (int base = start; base < p.V; base += W * kChunk) {
       float x[kPer];
       load_chunk(row, p.V, base, lane, x);
-      float top = x[0];
+      float top = fmaxf(x[0], -INFINITY);
 #pragma unroll
       for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[j]);
-      top = fmaxf(top, -INFINITY);  // of NaNs alone
-      if (p.k) best_take<T>(b, x, top, base, p.k, lane, first);
-      stat_take(s, x, top);
-      first = false;
+      const float chunk_top = wave_max(top);
+      if (p.k) best_take<T>(b, x, top, chunk_top, base, p.k, lane, base == start);
+      wave_stat_take(ws, x, top, chunk_top);
     }
   }
-  stat_wave(s);
-  if (p.k) best_shrink(b, p.k, lane);
-  float v = -INFINITY;
-  int id = -1;
+  Stat s = wave_stat_done(ws);
+  if (p.k && (b.count > 0 || W == 1)) best_shrink(b, p.k, lane);
+  int v = kNone, id = -1;
   if (W > 1) {
     if (lane == 0) {
       s_stat[wave] = s;
@@ -226,17 +252,16 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs 
     s = lane < W ? s_stat[lane] : stat_none();
     stat_wave(s);
     if (p.k) {
-      float ev[2];
-      int ei[2];
+      int ev[2], ei[2];
       for (int q = 0; q < 2; ++q) {
         const int w = (lane + 64 * q) / FUSION_MAX_K, at = (lane + 64 * q) % FUSION_MAX_K;
         const bool has = w < W && at < s_count[w < W ? w : 0];
-        ev[q] = has ? s_val[w][at] : -INFINITY;
+        ev[q] = has ? s_val[w][at] : kNone;
         ei[q] = has ? s_id[w][at] : INT_MAX;
       }
       pick_best(ev[0], ei[0], ev[1], ei[1], p.k, lane, v, id);
     }
-  } else if (p.k && lane < b.count) {
+  } else if (lane < b.count) {
     v = b.val[lane];
     id = b.id[lane];
   }
@@ -246,7 +271,7 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs 
   if (lane < p.k) {
     const bool none = dead || q.bad || id < 0;
     p.top_tokens[(int64_t)m * p.k + lane] = none ? -1 : id;
-    p.top_logp[(int64_t)m * p.k + lane] = r == -2 || (!dead && q.bad) ? nan : none ? -INFINITY : row_logp(q, v);
+    p.top_logp[(int64_t)m * p.k + lane] = r == -2 || (!dead && q.bad) ? nan : none ? -INFINITY : row_logp(q, of_order(v));
   }
   if (lane == 0) {
     if (p.logp) p.logp[m] = bad ? nan : dead || tok < 0 ? 0.0f : row_logp(q, x_tok);
@@ -262,21 +287,19 @@ struct GradArgs {
   const float *logp, *entropy, *lse, *g_logp, *g_entropy;
   void *grad;
   int64_t stride, g_stride;
-  int32_t M, B, V;
+  int32_t M, B, V, parts;  // parts: waves a row
 };
 
-// a wave a row and chunk of 1024 columns
+// A wave takes every parts-th chunk of 1024 columns of a row
 template <class T>
 __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
   constexpr int n = Pack<T>::n;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int chunks = (p.V + kChunk - 1) / kChunk;
   const int64_t job = (int64_t)blockIdx.x * 4 + wave;
-  if (job >= (int64_t)p.M * chunks) return;
-  const int r = (int)(job / chunks), base = (int)(job % chunks) * kChunk;
+  if (job >= (int64_t)p.M * p.parts) return;
+  const int r = (int)(job / p.parts), part = (int)(job % p.parts);
   const T *row = static_cast<const T *>(p.logits) + r * p.stride;
   T *out = static_cast<T *>(p.grad) + r * p.g_stride;
-  const bool whole = base + kChunk <= p.V;
 
   // The tokens chosen on this row: lane i looks at slot i of the row's stream
   const int slots = p.parents ? p.B : 1, first = p.parents ? r / p.B * p.B : r;
@@ -288,81 +311,101 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
     mine = par == r - first;
   }
   int tok = -1;
-  float gl = 0.0f, ge = 0.0f, lp_tok = 0.0f;
+  float gl = 0.0f, ge = 0.0f, lp_tok = 0.0f, lse = 0.0f, H = 0.0f;
   if (mine) {
-    if (p.tokens) tok = p.tokens[at];
-    if (tok < -1 || tok >= p.V) {
-      bad = true;
-      tok = -1;
-    }
-    if (tok >= 0 && p.g_logp) {
+    lse = p.lse[at];
+    if (p.g_logp) {
+      tok = p.tokens[at];
       gl = p.g_logp[at];
       lp_tok = p.logp[at];
-    } else {
-      tok = -1;
     }
-    if (p.g_entropy) ge = p.g_entropy[at];
+    if (p.g_entropy) {
+      ge = p.g_entropy[at];
+      H = p.entropy[at];
+    }
+    if (tok < 0 || tok >= p.V) {
+      bad |= tok != -1;
+      tok = -1;
+      gl = 0.0f;
+    }
   }
   const unsigned long long any = __ballot(mine);
   if (__ballot(bad) && lane == 0) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
-  float lse = 0.0f, H = 0.0f;
-  if (any) {
-    const int q = first + __builtin_ctzll(any);
-    lse = p.lse[q];
-    if (p.g_entropy) H = p.entropy[q];
-  }
+  const int one = any ? __builtin_ctzll(any) : 0;  // the row's statistics are the same for all its tokens
+  lse = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lse), one));
+  H = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(H), one));
   const float GL = wave_add(gl), GE = wave_add(ge);
   const bool nothing = !any || lse == -INFINITY;  // an empty row's outputs are constant
 
-  float x[kPer];
-  if (nothing) {
+  for (int base = part * kChunk; base < p.V; base += p.parts * kChunk) {
+    const bool whole = base + kChunk <= p.V;
+    float x[kPer];
+    if (nothing) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) x[j] = 0.0f;
-  } else {
-    if (whole) {
-      Pack<T> q[kPer / n];
-#pragma unroll
-      for (int i = 0; i < kPer / n; ++i) __builtin_memcpy(&q[i], row + base + (i * 64 + lane) * n, 16);
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) x[j] = to_float(q[j / n].v[j % n]);
+      for (int j = 0; j < kPer; ++j) x[j] = 0.0f;
     } else {
+      if (whole) {
+        Pack<T> q[kPer / n];
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const int c = column<T>(base, lane, j);
-        x[j] = c < p.V ? to_float(row[c]) : -INFINITY;
+        for (int i = 0; i < kPer / n; ++i) __builtin_memcpy(&q[i], row + base + (i * 64 + lane) * n, 16);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) x[j] = to_float(q[j / n].v[j % n]);
+      } else {
+        // (a lane reads its own columns alone: where the gradient is written in
+        // place, others are already overwritten)
+#pragma unroll
+        for (int i = 0; i < kPer / n; ++i) {
+          const int c = base + (i * 64 + lane) * n;
+          if (c + n <= p.V) {
+            Pack<T> q;
+            __builtin_memcpy(&q, row + c, 16);
+#pragma unroll
+            for (int e = 0; e < n; ++e) x[i * n + e] = to_float(q.v[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < n; ++e) x[i * n + e] = c + e < p.V ? to_float(row[c + e]) : -INFINITY;
+          }
+        }
+      }
+      if (GE == 0.0f) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) x[j] = -exp_of(x[j] - lse) * GL;
+      } else {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const float lp = x[j] - lse;
+          x[j] = -exp_of(lp) * (GL + GE * (fmaxf(lp, kFar) + H));
+        }
+      }
+      // the tokens' own columns, from their log probabilities: 1 - p is lost in x - lse where p is near 1
+      unsigned long long todo = __ballot(tok >= base && tok < base + kChunk);
+      while (todo) {
+        const int i = __builtin_ctzll(todo);
+        const int y = __builtin_amdgcn_readlane(tok, i);
+        const float lp = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lp_tok), i));
+        const bool same = tok == y;
+        const float own = wave_add(same ? gl : 0.0f), others = wave_add(same ? 0.0f : gl);
+        const float e = exp_of(lp), g = own * -expm1f(lp) - e * (others + GE * (fmaxf(lp, kFar) + H));
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+          if (column<T>(base, lane, j) == y) x[j] = g;
+        todo &= ~__ballot(same);
       }
     }
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const float lp = x[j] - lse, e = exp_of(lp);
-      x[j] = -e * (GL + GE * (fmaxf(lp, kFar) + H));
-    }
-    // the tokens' own columns, from their log probabilities: 1 - p is lost in x - lse where p is near 1
-    unsigned long long todo = __ballot(tok >= base && tok < base + kChunk);
-    while (todo) {
-      const int i = __builtin_ctzll(todo);
-      const int y = __builtin_amdgcn_readlane(tok, i);
-      const float lp = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lp_tok), i));
-      const bool same = tok == y;
-      const float own = wave_add(same ? gl : 0.0f), others = wave_add(same ? 0.0f : gl);
-      const float e = exp_of(lp), g = own * -expm1f(lp) - e * (others + GE * (fmaxf(lp, kFar) + H));
+    for (int i = 0; i < kPer / n; ++i) {
+      const int c = base + (i * 64 + lane) * n;
+      if (whole || c + n <= p.V) {
+        Pack<T> q;
 #pragma unroll
-      for (int j = 0; j < kPer; ++j)
-        if (column<T>(base, lane, j) == y) x[j] = g;
-      todo &= ~__ballot(same);
-    }
-  }
-  if (whole) {
-    Pack<T> q[kPer / n];
+        for (int e = 0; e < n; ++e) from_float(x[i * n + e], q.v[e]);
+        // (streaming: nothing reads it back soon)
+        __builtin_nontemporal_store(__builtin_bit_cast(Words, q), reinterpret_cast<UnalignedWords *>(out + c));
+      } else {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) from_float(x[j], q[j / n].v[j % n]);
-#pragma unroll
-    for (int i = 0; i < kPer / n; ++i) __builtin_memcpy(out + base + (i * 64 + lane) * n, &q[i], 16);
-  } else {
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int c = column<T>(base, lane, j);
-      if (c < p.V) from_float(x[j], out[c]);
+        for (int e = 0; e < n; ++e)
+          if (c + e < p.V) from_float(x[i * n + e], out[c + e]);
+      }
     }
   }
 }
@@ -382,6 +425,7 @@ int score_status_take(int32_t *bits) {
 
 namespace {
 constexpr int64_t kMaxRows = (1 << 24) - 1;
+constexpr int64_t kGradWaves = 1 << 16;  // enough to fill the chip several times
 // the checks that scoring and its gradient share
 int check_rows(int32_t dtype, int64_t stride, int32_t T, int32_t S, int32_t B, int32_t V, const void *parents) {
   if (dtype != FUSION_F32 && dtype != FUSION_BF16 && dtype != FUSION_F16) return set_error(FUSION_E_ARG, "unknown dtype");
@@ -419,10 +463,21 @@ extern "C" int token_logprobs(const void *logits, int32_t dtype, int64_t stride,
                     B, V, k};
   auto go = [&](auto type) {
     using T_ = decltype(type);
-    if (M >= 4096 || V <= kChunk)
+    // Waves a row, enough rows or chunks to fill the chip (us; fp32, 4 alternatives):
+    //                 1      4      8      16
+    //    6000 x 2500  17.4   27.2                 (a wave alone joins nothing)
+    //    3000 x 4096  13.7   17.8
+    //    3000 x 8190  23.3   24.1                 (35.4 and 29.4 with 8 alternatives)
+    //    1500 x 8190         12.9   16.4          (bf16)
+    //    600 x 8190          9.4    9.5    14.5
+    //    300 x 32000         19.9   15.4   18.0
+    //    513 x 100003        54     40     50     (bf16)
+    if (M >= 4096 || (M >= 2048 && V <= 4 * kChunk) || V <= kChunk)
       hipLaunchKernelGGL((score_kernel<T_, 1>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, stream, p);
     else if (M >= 1024 || V <= 4 * kChunk)
       hipLaunchKernelGGL((score_kernel<T_, 4>), dim3((unsigned)M), dim3(256), 0, stream, p);
+    else if (M >= 256 || V <= 8 * kChunk)
+      hipLaunchKernelGGL((score_kernel<T_, 8>), dim3((unsigned)M), dim3(512), 0, stream, p);
     else
       hipLaunchKernelGGL((score_kernel<T_, 16>), dim3((unsigned)M), dim3(1024), 0, stream, p);
   };
@@ -451,10 +506,11 @@ extern "C" int token_logprobs_backward(const void *logits, int32_t dtype, int64_
   if (grad_logp && (!tokens || !logp)) return set_error(FUSION_E_ARG, "gradient of the log probabilities without tokens or logp");
   if (grad_entropy && !entropy) return set_error(FUSION_E_ARG, "gradient of the entropy without entropy");
   if (logits == grad_logits && stride != grad_stride) return set_error(FUSION_E_ARG, "in place with another stride");
-  const int64_t blocks = (M * ((V + kChunk - 1) / kChunk) + 3) / 4;
-  if (blocks >= 1 << 24) return set_error(FUSION_E_UNSUPPORTED, "too many rows: split the call along T");
+  const int chunks = (V + kChunk - 1) / kChunk;
+  const int parts = (int)std::min<int64_t>(chunks, std::max<int64_t>(1, kGradWaves / M));
+  const int64_t blocks = (M * parts + 3) / 4;
   const GradArgs p{logits, tokens, parents, logp, entropy, lse, grad_logp, grad_entropy, grad_logits, stride, grad_stride,
-                   (int32_t)M, B, V};
+                   (int32_t)M, B, V, parts};
   const dim3 grid((unsigned)blocks), block(256);
   if (dtype == FUSION_F32) hipLaunchKernelGGL(grad_kernel<float>, grid, block, 0, stream, p);
   else if (dtype == FUSION_BF16) hipLaunchKernelGGL(grad_kernel<Brain>, grid, block, 0, stream, p);

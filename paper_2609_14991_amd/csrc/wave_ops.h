@@ -30,11 +30,17 @@ __device__ __forceinline__ int wave_reduce(int ident, int v, F op) {
   v = op(v, wave_move<0x143, 0xC>(ident, v));
   return __builtin_amdgcn_readlane(v, 63);
 }
-__device__ __forceinline__ float wave_max(float x) {
-  return __int_as_float(wave_reduce(__float_as_int(-INFINITY), __float_as_int(x), [](int a, int b) {
-    return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b)));
-  }));
+// Order-preserving image of a float that is not NaN, the zeros as one, and back.
+// (Integer maxima and minima take their neighbour's value in the same instruction.)
+__device__ __forceinline__ int order_of(float x) {
+  const int b = __float_as_int(x + 0.0f);
+  return b ^ ((b >> 31) & 0x7FFFFFFF);
 }
+__device__ __forceinline__ float of_order(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7FFFFFFF)); }
+__device__ __forceinline__ int wave_max(int x) {
+  return wave_reduce(INT_MIN, x, [](int a, int b) { return max(a, b); });
+}
+__device__ __forceinline__ float wave_max(float x) { return of_order(wave_max(order_of(x))); }
 __device__ __forceinline__ float wave_add(float x) {
   return __int_as_float(wave_reduce(0, __float_as_int(x), [](int a, int b) {
     return __float_as_int(__int_as_float(a) + __int_as_float(b));
@@ -91,6 +97,59 @@ __device__ __forceinline__ void stat_take(Stat &s, const float (&x)[n], float la
     s.rest += d == 0.0f ? 0.0f : e;
     s.u = fmaf(fmaxf(d, kFar), e, s.u);
   }
+}
+
+// Statistics that a wave gathers over a row: relative to a maximum that its lanes
+// share, the sums a lane's own; u in units of log2 e.  The maxima are among the rest
+// as long as that is 1.25 or more, and counted as ones where it would be less.
+struct WaveStat {
+  float m, ones, rest, u;
+};
+__device__ __forceinline__ WaveStat wave_stat_none() { return WaveStat{-INFINITY, 0.0f, 0.0f, 0.0f}; }
+
+// x - base in units of log2 e, kFar for -infinity (NaN stays)
+__device__ __forceinline__ float log2_of(float x, float base) {
+  return __builtin_elementwise_maximum((x - base) * kLog2e, kFar);
+}
+
+// `n` more values of every lane; top: the lane's largest, all_top: the wave's.  Six
+// operations a value, the exponential among them.
+template <int n>
+__device__ __forceinline__ void wave_stat_take(WaveStat &s, const float (&x)[n], float top, float all_top) {
+  if (all_top > s.m) {  // uniform
+    const float d = fmaxf((s.m - all_top) * kLog2e, kFar), f = __builtin_amdgcn_exp2f(d), all = s.ones + s.rest;
+    s.u = f * (s.u + d * all);
+    s.rest = f * all;
+    s.ones = 0.0f;
+    s.m = all_top;
+  }
+  const float base = s.m == -INFINITY ? 0.0f : s.m;
+  float sum[4] = {}, u[4] = {};
+#pragma unroll
+  for (int j = 0; j < n; ++j) {
+    const float t = log2_of(x[j], base), e = __builtin_amdgcn_exp2f(t);
+    sum[j % 4] += e;
+    u[j % 4] = fmaf(t, e, u[j % 4]);
+  }
+  const float more = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  // the maximum is new, and next to nothing with it: its 1 apart
+  if (all_top == s.m && all_top != -INFINITY && __ballot(top == s.m && more < 1.25f) && wave_add(more) < 1.25f) {
+#pragma unroll
+    for (int j = 0; j < n; ++j) {
+      const float t = log2_of(x[j], base), e = x[j] == s.m ? 0.0f : __builtin_amdgcn_exp2f(t);
+      s.ones += x[j] == s.m ? 1.0f : 0.0f;
+      s.rest += e;
+      s.u = fmaf(t, e, s.u);
+    }
+  } else {
+    s.rest += more;
+    s.u += (u[0] + u[1]) + (u[2] + u[3]);
+  }
+}
+
+// the lanes' together, in every lane
+__device__ __forceinline__ Stat wave_stat_done(const WaveStat &s) {
+  return Stat{s.m, wave_add(s.ones), wave_add(s.rest), wave_add(s.u * kLn2)};
 }
 
 // two sets' statistics as one
