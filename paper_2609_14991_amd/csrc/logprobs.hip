@@ -116,7 +116,22 @@ __device__ __forceinline__ void best_shrink(Best &b, int k, int lane) {
   const int v0 = h0 ? b.val[lane] : kNone, v1 = h1 ? b.val[lane + 64] : kNone;
   const int i0 = h0 ? b.id[lane] : INT_MAX, i1 = h1 ? b.id[lane + 64] : INT_MAX;
   int v, id;
-  pick_best(v0, i0, v1, i1, k, lane, v, id);
+  if (b.count <= 24) {
+    // few: each counts those before it, a third of a round of pick_best a candidate
+    int rank = 0;
+    for (int c = 0; c < b.count; ++c)
+      rank += before(__builtin_amdgcn_readlane(v0, c), __builtin_amdgcn_readlane(i0, c), v0, i0) ? 1 : 0;
+    wave_lds_sync();
+    if (h0) {
+      b.val[rank] = v0;
+      b.id[rank] = i0;
+    }
+    wave_lds_sync();
+    v = b.val[lane];
+    id = b.id[lane];
+  } else {
+    pick_best(v0, i0, v1, i1, k, lane, v, id);
+  }
   wave_lds_sync();
   b.count = min(b.count, k);
   if (lane < b.count) {
