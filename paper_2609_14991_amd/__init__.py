@@ -375,12 +375,17 @@ def _dtype(t) -> int:
     return _DTYPES.get(t.dtype, -1)
 
 
+def _at(t):
+    """A tensor's device address as a plain int (ctypes turns it into the pointer), None for None."""
+    return None if t is None else t.data_ptr()
+
+
 def token_logprobs(logits, stride, T, S, B, V, tokens, parents, k, logp, entropy, lse, top_tokens=None, top_logp=None,
                    stream=None):
     """Same arguments as the C call, the dtype taken from logits; CUDA (HIP) tensors, float32 outputs."""
-    _check(lib().token_logprobs(_ptr(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V), _ptr(tokens),
-                                _ptr(parents), int(k), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(top_tokens),
-                                _ptr(top_logp), _stream(stream)))
+    _check(lib().token_logprobs(_at(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V), _at(tokens),
+                                _at(parents), int(k), _at(logp), _at(entropy), _at(lse), _at(top_tokens),
+                                _at(top_logp), _stream(stream)))
 
 
 def token_logprobs_backward(logits, stride, T, S, B, V, tokens, parents, logp, entropy, lse, grad_logp, grad_entropy,
@@ -388,9 +393,9 @@ def token_logprobs_backward(logits, stride, T, S, B, V, tokens, parents, logp, e
     """Same arguments as the C call, the dtype taken from logits (grad_logits has the same); CUDA (HIP) tensors."""
     if grad_logits.dtype != logits.dtype:
         raise ValueError("grad_logits must have the type of logits")
-    _check(lib().token_logprobs_backward(_ptr(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V),
-                                         _ptr(tokens), _ptr(parents), _ptr(logp), _ptr(entropy), _ptr(lse),
-                                         _ptr(grad_logp), _ptr(grad_entropy), _ptr(grad_logits), int(grad_stride),
+    _check(lib().token_logprobs_backward(_at(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V),
+                                         _at(tokens), _at(parents), _at(logp), _at(entropy), _at(lse),
+                                         _at(grad_logp), _at(grad_entropy), _at(grad_logits), int(grad_stride),
                                          _stream(stream)))
 
 
@@ -403,8 +408,8 @@ def joint_logprobs_workspace(M, V, K) -> int:
 
 def joint_logprobs(A, W, bias, K, T, S, B, V, tokens, parents, logp, entropy, lse, workspace, stream=None):
     """Same arguments as the C call (the workspace's size is its tensor's); A and W bfloat16 (or int16 bit patterns)."""
-    _check(lib().joint_logprobs(_ptr(A), _ptr(W), _ptr(bias), int(K), int(T), int(S), int(B), int(V), _ptr(tokens),
-                                _ptr(parents), _ptr(logp), _ptr(entropy), _ptr(lse), _ptr(workspace),
+    _check(lib().joint_logprobs(_at(A), _at(W), _at(bias), int(K), int(T), int(S), int(B), int(V), _at(tokens),
+                                _at(parents), _at(logp), _at(entropy), _at(lse), _at(workspace),
                                 workspace.numel(), _stream(stream)))
 
 
@@ -415,19 +420,19 @@ def mx_scale_stride(K) -> int:
 
 def mx_quantize(x, stride, R, K, q, scales, stream=None):
     """Same arguments as the C call, the dtype taken from x; q [R, K // 2] and scales [R, mx_scale_stride(K)] uint8."""
-    _check(lib().mx_quantize(_ptr(x), _dtype(x), int(stride), int(R), int(K), _ptr(q), _ptr(scales), _stream(stream)))
+    _check(lib().mx_quantize(_at(x), _dtype(x), int(stride), int(R), int(K), _at(q), _at(scales), _stream(stream)))
 
 
 def mx_dequantize(q, scales, R, K, out, stride, stream=None):
     """Same arguments as the C call, the dtype taken from out."""
-    _check(lib().mx_dequantize(_ptr(q), _ptr(scales), int(R), int(K), _ptr(out), _dtype(out), int(stride),
+    _check(lib().mx_dequantize(_at(q), _at(scales), int(R), int(K), _at(out), _dtype(out), int(stride),
                                _stream(stream)))
 
 
 def joint_project_mx(A, A_scales, W, W_scales, bias, M, N, K, out, stream=None):
     """Same arguments as the C call; operands as mx_quantize writes them, bias and out float32 CUDA tensors."""
-    _check(lib().joint_project_mx(_ptr(A), _ptr(A_scales), _ptr(W), _ptr(W_scales), _ptr(bias), int(M), int(N), int(K),
-                                  _ptr(out), _stream(stream)))
+    _check(lib().joint_project_mx(_at(A), _at(A_scales), _at(W), _at(W_scales), _at(bias), int(M), int(N), int(K),
+                                  _at(out), _stream(stream)))
 
 
 def fusion_device_status(stream=None) -> int:
@@ -465,6 +470,132 @@ def project(A, W, bias=None, stream=None):
     N = W.shape[0]
     out = torch.empty((M, N), dtype=torch.float32, device=A.device)
     joint_project(A, W, bias, M, N, K, out, stream)
+    return out
+
+
+def _want(t, what, dtype, shape):
+    """A device tensor of this type and shape (None in a shape: any size), its elements in order."""
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or len(t.shape) != len(shape) or any(
+            n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what}: a contiguous CUDA tensor of {dtype}, shape {list(shape)}, is wanted")
+    return t
+
+
+def _rows(logits, what="logits"):
+    """T, H, V and the distance of the rows of logits [T, H, V], which may lie apart."""
+    if not logits.is_cuda or logits.dim() != 3 or _dtype(logits) < 0:
+        raise ValueError(f"{what}: a CUDA tensor [T, S * B, V] of float32, bfloat16 or float16 is wanted")
+    T, H, V = logits.shape
+    # (a dimension of one row says nothing about their distance)
+    stride = logits.stride(1) if H > 1 else logits.stride(0) if T > 1 else V
+    if logits.numel() and ((V > 1 and logits.stride(2) != 1) or stride < V or (T > 1 and logits.stride(0) != H * stride)):
+        raise ValueError(f"{what}: rows one distance apart, each in order, are wanted")
+    return T, H, V, stride
+
+
+def score(logits, tokens=None, parents=None, B=1, k=0, stream=None):
+    """Log probabilities [T, S * B] of the tokens that a decode (``run``) chose from logits [T, S * B, V],
+    the entropies and log sum exps of the rows they were chosen on, and the k best alternatives
+    ``top`` and ``top_logp`` [T, S * B, k].  Without tokens the rows alone."""
+    import torch
+
+    T, H, V, stride = _rows(logits)
+    if H % B != 0:
+        raise ValueError("S * B rows a frame are wanted")
+    for t, what in ((tokens, "tokens"), (parents, "parents")):
+        if t is not None:
+            _want(t, what, torch.int32, (T, H))
+    new = lambda dt, *n: torch.empty((T, H) + n, dtype=dt, device=logits.device)  # noqa: E731
+    out = dict(logp=None if tokens is None else new(torch.float32), entropy=new(torch.float32), lse=new(torch.float32),
+               top=new(torch.int32, k) if k else None, top_logp=new(torch.float32, k) if k else None)
+    token_logprobs(logits, stride, T, H // B, B, V, tokens, parents, k, out["logp"], out["entropy"], out["lse"], out["top"],
+                   out["top_logp"], stream)
+    return out
+
+
+def score_backward(logits, scored, tokens=None, parents=None, B=1, grad_logp=None, grad_entropy=None, in_place=False,
+                   stream=None):
+    """The gradient with respect to logits of what ``score`` gave (``scored``) for the same arguments, of the
+    logits' type; ``in_place`` writes it over them."""
+    import torch
+
+    T, H, V, stride = _rows(logits)
+    if H % B != 0:
+        raise ValueError("S * B rows a frame are wanted")
+    for t, what, dt in ((tokens, "tokens", torch.int32), (parents, "parents", torch.int32), (grad_logp, "grad_logp", torch.float32),
+                        (grad_entropy, "grad_entropy", torch.float32)):
+        if t is not None:
+            _want(t, what, dt, (T, H))
+    for n in ("logp", "entropy", "lse"):
+        if scored[n] is not None:
+            _want(scored[n], n, torch.float32, (T, H))
+    grad = logits if in_place else torch.empty((T, H, V), dtype=logits.dtype, device=logits.device)
+    token_logprobs_backward(logits, stride, T, H // B, B, V, tokens, parents, scored["logp"], scored["entropy"], scored["lse"],
+                            grad_logp, grad_entropy, grad, stride if in_place else V, stream)
+    return grad
+
+
+def score_projected(A, W, bias=None, tokens=None, parents=None, B=1, stream=None):
+    """``score`` (without alternatives) straight from the hidden states A [T, S * B, K] and the output layer
+    W [V, K] (bf16) and bias: the logits are never stored."""
+    import torch
+
+    T, H, K = A.shape
+    V = W.shape[0]
+    _want(A, "A", torch.bfloat16, (None, None, K))
+    _want(W, "W", torch.bfloat16, (None, K))
+    if bias is not None:
+        _want(bias, "bias", torch.float32, (V,))
+    if H % B != 0:
+        raise ValueError("S * B rows a frame are wanted")
+    for t, what in ((tokens, "tokens"), (parents, "parents")):
+        if t is not None:
+            _want(t, what, torch.int32, (T, H))
+    new = lambda: torch.empty((T, H), dtype=torch.float32, device=A.device)  # noqa: E731
+    out = dict(logp=None if tokens is None else new(), entropy=new(), lse=new())
+    work = torch.empty(joint_logprobs_workspace(T * H, V, K), dtype=torch.float32, device=A.device)
+    joint_logprobs(A, W, bias, K, T, H // B, B, V, tokens, parents, out["logp"], out["entropy"], out["lse"], work, stream)
+    return out
+
+
+def quantize(x, stream=None):
+    """x [R, K] (float32, bfloat16 or float16; rows may lie apart) in microscaled 4-bit floating point: the
+    packed elements [R, K // 2] and scale bytes [R, mx_scale_stride(K)], both uint8."""
+    import torch
+
+    _, R, K, stride = _rows(x.unsqueeze(0) if x.dim() == 2 else x, "x")
+    q = torch.empty((R, K // 2), dtype=torch.uint8, device=x.device)
+    s = torch.empty((R, mx_scale_stride(K)), dtype=torch.uint8, device=x.device)
+    mx_quantize(x, stride, R, K, q, s, stream)
+    return q, s
+
+
+def dequantize(q, scales, dtype=None, stream=None):
+    """The values [R, K] that ``quantize``'s result stands for, float32 or another type."""
+    import torch
+
+    R, K = q.shape[0], 2 * q.shape[1]
+    _want(q, "q", torch.uint8, (R, K // 2))
+    _want(scales, "scales", torch.uint8, (R, mx_scale_stride(K)))
+    out = torch.empty((R, K), dtype=torch.float32 if dtype is None else dtype, device=q.device)
+    mx_dequantize(q, scales, R, K, out, K, stream)
+    return out
+
+
+def project_mx(A, W, bias=None, stream=None):
+    """``project`` with both operands as ``quantize`` gives them; A may also be the states [M, K] themselves,
+    which are then quantised first."""
+    import torch
+
+    (qw, sw), (qa, sa) = W, A if isinstance(A, tuple) else quantize(A, stream)
+    M, N, K = qa.shape[0], qw.shape[0], 2 * qw.shape[1]
+    for t, what, shape in ((qa, "A", (M, K // 2)), (sa, "A's scales", (M, mx_scale_stride(K))), (qw, "W", (N, K // 2)),
+                           (sw, "W's scales", (N, mx_scale_stride(K)))):
+        _want(t, what, torch.uint8, shape)
+    if bias is not None:
+        _want(bias, "bias", torch.float32, (N,))
+    out = torch.empty((M, N), dtype=torch.float32, device=qa.device)
+    joint_project_mx(qa, sa, qw, sw, bias, M, N, K, out, stream)
     return out
 
 

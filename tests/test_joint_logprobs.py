@@ -149,6 +149,54 @@ def test_the_token_logit_is_the_one_in_the_statistics():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V", [40, 700, 4100])
+def test_masked_tokens(V):
+    """A bias of -inf masks tokens: some, all but one, all; a NaN breaks every row."""
+    rng = np.random.default_rng(V)
+    M, K = 40, 72
+    A, W, bias = _joint(rng, M, V, K)
+    tok = rng.integers(0, V, (1, M))
+    bias[rng.random(V) < 0.9] = -np.inf
+    tok[0, :5] = np.flatnonzero(np.isfinite(bias))[:5] if np.isfinite(bias).sum() >= 5 else 0
+    got = _run(A, W, bias, 1, M, 1, tok, None)
+    x = projection.joint_project(A, W, bias)[None]
+    ref = O.scores(x, tok, None, M, 1, 0)
+    d = projection.fp32_error_bound(A, W, np.where(np.isfinite(bias), bias, 0)).max()
+    for n in ("logp", "lse", "entropy"):
+        same = got[n] == ref[n]
+        assert np.all(same | (np.abs(np.where(same, 0, got[n]) - np.where(same, 0, ref[n])) <= 2 * ref["tol_" + n] + 1e-5 + 16 * d)), n
+    assert (got["logp"] == -np.inf).any()
+    one = np.full(V, -np.inf, dtype=np.float32)
+    one[V // 2] = 1.0
+    got = _run(A, W, one, 1, M, 1, np.full((1, M), V // 2), None)
+    assert (got["logp"] == 0).all() and (got["entropy"] == 0).all() and np.isfinite(got["lse"]).all()
+    got = _run(A, W, np.full(V, -np.inf, dtype=np.float32), 1, M, 1, tok, None)
+    assert (got["logp"] == -np.inf).all() and (got["lse"] == -np.inf).all() and (got["entropy"] == 0).all()
+    one[V - 1] = np.nan
+    got = _run(A, W, one, 1, M, 1, tok, None)
+    assert all(np.isnan(got[n]).all() for n in got)
+
+
+@pytest.mark.gpu
+def test_confident_rows_from_hidden_states():
+    """One token far above the rest: -log p is the rest's sum, whose terms' differences the logits' errors bound."""
+    rng = np.random.default_rng(14)
+    M, V, K = 70, 1000, 128
+    A, W, _ = _joint(rng, M, V, K, scale=1.0)
+    x = projection.joint_project(A, W)
+    for gap in (6.0, 10.0, 16.0):
+        bias = np.zeros(V, dtype=np.float32)
+        bias[33] = gap + 6.0
+        tok = np.full((1, M), 33)
+        got = _run(A, W, bias, 1, M, 1, tok, None)
+        ref = O.scores(projection.joint_project(A, W, bias)[None], tok, None, M, 1, 0)
+        d = projection.fp32_error_bound(A, W, bias).max()
+        # each term of the rest off by a factor of e^(2 d), and the sums' roundings (1/16 of a part is held to 1e-5)
+        assert np.all(np.abs(got["logp"] - ref["logp"]) <= (2.5 * d + 2e-5) * np.abs(ref["logp"]))
+    assert x.shape == (M, V)
+
+
+@pytest.mark.gpu
 def test_bad_tokens_and_missing_outputs():
     rng = np.random.default_rng(12)
     A, W, bias = _joint(rng, 8, 50, 64)
@@ -291,6 +339,64 @@ def test_scores_after_a_projected_decode(k):
         assert torch.equal(live, torch.isfinite(u))
         # two evaluations of each logit, and 200 roundings of either sum
         assert ((u - v).abs()[live] <= 2 * d * 14 + 400 * O.U32 * 14).all()  # entropy at most log 600 < 7, twice
+
+
+@pytest.mark.gpu
+def test_conveniences_equal_the_calls():
+    rng = np.random.default_rng(33)
+    T, S, B, V, K, k = 3, 4, 2, 300, 96, 3
+    H = S * B
+    A, W = torch.tensor(rng.standard_normal((T, H, K))).bfloat16().to(dev()), torch.tensor(rng.standard_normal((V, K)) / 5).bfloat16().to(dev())
+    bias = torch.tensor(rng.standard_normal(V), dtype=torch.float32, device=dev())
+    tok_np, par_np = _decoded(rng, T, S, B, V)
+    tok, par = _up(tok_np, np.int32), _up(par_np, np.int32)
+    logits = F.project(A.view(T * H, K), W, bias).view(T, H, V)
+    o = F.score(logits, tok, par, B, k)
+    raw = [torch.empty((T, H), device=dev()) for _ in range(3)] + [torch.empty((T, H, k), dtype=torch.int32, device=dev()), torch.empty((T, H, k), device=dev())]
+    F.token_logprobs(logits, V, T, S, B, V, tok, par, k, *raw)
+    for n, r in zip(("logp", "entropy", "lse", "top", "top_logp"), raw):
+        assert torch.equal(o[n], r)
+    gl = torch.tensor(rng.standard_normal((T, H)), dtype=torch.float32, device=dev())
+    grad = F.score_backward(logits, o, tok, par, B, gl, gl)
+    wide = torch.zeros((T, H, V + 7), device=dev())
+    wide[:, :, :V] = logits
+    view = wide[:, :, :V]
+    assert torch.equal(F.score(view, tok, par, B)["logp"], o["logp"])
+    assert F.score_backward(view, o, tok, par, B, gl, gl, in_place=True) is view
+    assert torch.equal(view, grad) and (wide[:, :, V:] == 0).all()
+    raw = [torch.empty((T, H), device=dev()) for _ in range(3)]
+    F.joint_logprobs(A, W, bias, K, T, S, B, V, tok, par, *raw, torch.empty(F.joint_logprobs_workspace(T * H, V, K), device=dev()))
+    p = F.score_projected(A, W, bias, tok, par, B)
+    assert all(torch.equal(p[n], r) for n, r in zip(("logp", "entropy", "lse"), raw))
+    assert F.score(logits)["logp"] is None and F.score_projected(A, W)["logp"] is None
+    q, s = F.quantize(A.view(T * H, K))
+    wq = F.quantize(W)
+    x = F.project_mx(A.view(T * H, K), wq, bias)
+    assert torch.equal(x, F.project_mx((q, s), wq, bias))
+    ref = F.dequantize(q, s).double() @ F.dequantize(*wq).double().T + bias.double()
+    assert (x.double() - ref).abs().max() <= 2 * K * O.U32 * (ref.abs().max() + K * 36)
+    assert F.dequantize(q, s, torch.bfloat16).dtype == torch.bfloat16
+
+
+def test_conveniences_refuse_what_the_calls_would_misread():
+    """CPU tensors, other types, other shapes and orders: refused before anything is launched."""
+    x, tok = torch.zeros((2, 4, 8)), torch.zeros((2, 4), dtype=torch.int32)
+    for call in (lambda: F.score(x, tok), lambda: F.score_projected(x.bfloat16(), torch.zeros((8, 8), dtype=torch.bfloat16)),
+                 lambda: F.quantize(torch.zeros((4, 32))), lambda: F.dequantize(torch.zeros((4, 16), dtype=torch.uint8), torch.zeros((4, 8), dtype=torch.uint8)),
+                 lambda: F.score_backward(x, dict(logp=None, entropy=None, lse=None), tok, None, 1, torch.zeros((2, 4)))):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.gpu
+def test_conveniences_refuse_other_types_shapes_and_orders():
+    x, tok = torch.zeros((2, 4, 8), device=dev()), torch.zeros((2, 4), dtype=torch.int32, device=dev())
+    for call in (lambda: F.score(x, tok.long()), lambda: F.score(x, tok[:, :2]), lambda: F.score(x, tok, B=3),
+                 lambda: F.score(x.transpose(1, 2)), lambda: F.score(x[:, ::2], tok[:, ::2]), lambda: F.score(x.double()),
+                 lambda: F.score(x, tok.t().contiguous().t()), lambda: F.quantize(x.to(torch.int32)),
+                 lambda: F.project_mx(F.quantize(torch.zeros((4, 64), device=dev())), F.quantize(torch.zeros((4, 32), device=dev())))):
+        with pytest.raises(ValueError):
+            call()
 
 
 @pytest.mark.gpu

@@ -263,9 +263,9 @@ def test_product_of_many_rows(M, N, K):
 
 
 @pytest.mark.gpu
-def test_product_ignores_bytes_behind_the_scales_and_spreads_nan():
+@pytest.mark.parametrize("M,N,K", [(40, 70, 352), (9000, 1000, 352)])
+def test_product_ignores_bytes_behind_the_scales_and_spreads_nan(M, N, K):
     rng = np.random.default_rng(5)
-    M, N, K = 40, 70, 352
     qa, sa, qw, sw, bias = _operands(rng, M, N, K)
     clean = _product(qa, sa, qw, sw, bias, K)
     sa[:, K // 32:], sw[:, K // 32:] = 255, 255
