@@ -220,7 +220,10 @@ struct ScoreArgs {
   int32_t M, B, V, k;
 };
 
-// W waves a token: 4 tokens a workgroup of 256 lanes with one wave each, else one.
+// W waves a row of logits: 4 rows a workgroup of 256 lanes with one wave each, else
+// one.  A row is looked at once for all the tokens that were chosen on it (a beam's
+// slots share parents: 300 frames of 64 x 4 slots with random parents are chosen on two
+// thirds of the rows, 185 us token by token and 166 so); a row nothing was chosen on is not.
 // (32 values a lane instead of 16: half the waves fit, 173 -> 204 us for 76800 rows
 // of 4096 in bf16 with 4 alternatives.)
 template <class T, int W>
@@ -231,35 +234,53 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs 
   __shared__ Stat s_stat[kWaves];
   __shared__ int s_count[kWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t token_at = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
-  if (token_at >= p.M) return;  // whole waves, and with W > 1 none
-  const int m = (int)token_at;
-  const int64_t r = row_of_token(p.parents, m, p.B);
-  const int tok = p.tokens ? p.tokens[m] : -1;
-  const bool bad_token = tok < -1 || tok >= p.V;
-  const bool dead = r < 0;
-  const T *row = static_cast<const T *>(p.logits) + (dead ? 0 : r) * p.stride;
+  const int64_t row_at = W == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  if (row_at >= p.M) return;  // whole waves, and with W > 1 none
+  const int r = (int)row_at;
+  const float nan = __int_as_float(0x7FC00000);
+
+  // The tokens chosen on this row: lane i looks at slot i of the row's stream
+  const int slots = p.parents ? p.B : 1, first = p.parents ? r / p.B * p.B : r, m = first + lane;
+  const T *row = static_cast<const T *>(p.logits) + r * p.stride;
+  int par = lane, tok = -1;
+  if (lane < slots) {
+    if (p.parents) par = p.parents[m];
+    if (p.tokens) tok = p.tokens[m];
+  }
+  const bool bad_token = tok < -1 || tok >= p.V, bad_parent = par < -1 || par >= slots;
+  const bool mine = lane < slots && (p.parents ? par == r - first : true);
+  const unsigned long long any = __ballot(mine);
+  if (p.parents && wave % W == 0 && lane == r - first && (par == -1 || bad_parent)) {
+    // the slot of the row's own number is dead: nobody else writes its outputs
+    if (p.logp) p.logp[r] = bad_token || bad_parent ? nan : 0.0f;
+    if (p.entropy) p.entropy[r] = bad_parent ? nan : 0.0f;
+    if (p.lse) p.lse[r] = bad_parent ? nan : -INFINITY;
+    for (int j = 0; j < p.k; ++j) {
+      p.top_tokens[(int64_t)r * p.k + j] = -1;
+      p.top_logp[(int64_t)r * p.k + j] = bad_parent ? nan : -INFINITY;
+    }
+    if (bad_token || bad_parent) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
+  }
+  if (!any) return;  // (the same in every wave of the row)
   float x_tok = 0.0f;
-  if (!dead && tok >= 0 && !bad_token) x_tok = to_float(row[tok]);
+  if (mine && wave % W == 0 && tok >= 0 && !bad_token) x_tok = to_float(row[tok]);
   WaveStat ws = wave_stat_none();
   Best b{s_val[wave], s_id[wave], 0, -INFINITY};
-  if (!dead) {
-    const int start = (W == 1 ? 0 : wave) * kChunk;
-    // Raising the floor now and then pays over 8 chunks or more with many alternatives
-    // (us, 8 of them: 513 x 100003 53 -> 45, 16000 x 8190 82 -> 75, but 3000 x 8190
-    // with 4 waves a row 27.1 -> 27.7), not where a row's own time counts (16 x 131072
-    // with 16 waves 23.6 -> 25.6)
-    const int trim = W <= 8 && p.k > 4 && p.V >= 8 * W * kChunk - kChunk / 2 ? 6 * p.k : kList;
-    for (int base = start; base < p.V; base += W * kChunk) {
-      float x[kPer];
-      load_chunk(row, p.V, base, lane, x);
-      float top = fmaxf(x[0], -INFINITY);
+  const int start = (W == 1 ? 0 : wave) * kChunk;
+  // Raising the floor now and then pays over 8 chunks or more with many alternatives
+  // (us, 8 of them: 513 x 100003 53 -> 45, 16000 x 8190 82 -> 75, but 3000 x 8190
+  // with 4 waves a row 27.1 -> 27.7), not where a row's own time counts (16 x 131072
+  // with 16 waves 23.6 -> 25.6)
+  const int trim = W <= 8 && p.k > 4 && p.V >= 8 * W * kChunk - kChunk / 2 ? 6 * p.k : kList;
+  for (int base = start; base < p.V; base += W * kChunk) {
+    float x[kPer];
+    load_chunk(row, p.V, base, lane, x);
+    float top = fmaxf(x[0], -INFINITY);
 #pragma unroll
-      for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[j]);
-      const float chunk_top = wave_max(top);
-      if (p.k) best_take<T>(b, x, top, chunk_top, base, p.k, trim, lane, base == start);
-      wave_stat_take(ws, x, top, chunk_top);
-    }
+    for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[j]);
+    const float chunk_top = wave_max(top);
+    if (p.k) best_take<T>(b, x, top, chunk_top, base, p.k, trim, lane, base == start);
+    wave_stat_take(ws, x, top, chunk_top);
   }
   Stat s = wave_stat_done(ws);
   if (p.k && (b.count > 0 || W == 1)) best_shrink(b, p.k, lane);
@@ -288,18 +309,22 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs 
     id = b.id[lane];
   }
   const RowScore q = row_score(s);
-  const float nan = __int_as_float(0x7FC00000);
-  const bool bad = bad_token || r == -2;
-  if (lane < p.k) {
-    const bool none = dead || q.bad || id < 0;
-    p.top_tokens[(int64_t)m * p.k + lane] = none ? -1 : id;
-    p.top_logp[(int64_t)m * p.k + lane] = r == -2 || (!dead && q.bad) ? nan : none ? -INFINITY : row_logp(q, of_order(v));
+  if (p.k) {
+    const int top = q.bad ? -1 : id;
+    const float top_logp = q.bad ? nan : id < 0 ? -INFINITY : row_logp(q, of_order(v));
+    for (unsigned long long todo = any; todo; todo &= todo - 1) {
+      const int64_t at = (int64_t)(first + __builtin_ctzll(todo)) * p.k + lane;
+      if (lane < p.k) {
+        p.top_tokens[at] = top;
+        p.top_logp[at] = top_logp;
+      }
+    }
   }
-  if (lane == 0) {
-    if (p.logp) p.logp[m] = bad ? nan : dead || tok < 0 ? 0.0f : row_logp(q, x_tok);
-    if (p.entropy) p.entropy[m] = r == -2 ? nan : q.entropy;
-    if (p.lse) p.lse[m] = r == -2 ? nan : q.lse;
-    if (bad) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
+  if (mine) {
+    if (p.logp) p.logp[m] = bad_token ? nan : tok < 0 ? 0.0f : row_logp(q, x_tok);
+    if (p.entropy) p.entropy[m] = q.entropy;
+    if (p.lse) p.lse[m] = q.lse;
+    if (bad_token) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
   }
 }
 
