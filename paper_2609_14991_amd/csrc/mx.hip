@@ -25,7 +25,10 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlock = 32;
 
-// A lane takes 16 bytes of a row, so 8 (fp32) or 4 lanes share a block
+// A lane takes 16 bytes of a row, so 8 (fp32) or 4 lanes share a block and find its
+// largest magnitude among themselves.  Bound by memory: 76800 x 640 in bf16 21 us (98 MB
+// in, 26 out, 5.9 TB/s), 38421 x 1184 in fp32 34 us (6.1 TB/s), 46 from rows not in
+// any cache.
 template <class T>
 __global__ void __launch_bounds__(256) quantize_kernel(const T *__restrict__ x, int64_t stride, uint32_t packs, uint32_t per_row,
                                                        int K, uint8_t *__restrict__ q, uint8_t *__restrict__ scales) {
@@ -71,7 +74,8 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T *__restrict__ x, 
   }
 }
 
-// a lane writes 16 bytes of a row
+// A lane writes 16 bytes of a row.  Bound by its stores: 38421 x 1184 in fp32 31 us,
+// 182 MB out, 6.7 TB/s with what it reads.
 template <class T>
 __global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ scales,
                                                          uint32_t packs, uint32_t per_row, int K, int64_t stride,
@@ -155,6 +159,9 @@ struct MxArgs {
   int M, N, K, n_col_tiles, map;
 };
 
+// Tile by tile, as joint_proj_kernel: for few tiles, where latency counts (256 x 4096
+// x 640: 5.4 us), and for a K that mx_panel_kernel's registers do not hold.  A large
+// output it writes at 4.3 TB/s (290 us for 76800 x 4096 x 640: operands 170, stores 190).
 template <class S, int kAux>
 __global__ void __launch_bounds__(64 * S::waves, 2) mx_proj_kernel(MxArgs p) {
   __shared__ __align__(1024) unsigned char smem[S::lds];
@@ -179,6 +186,8 @@ __global__ void __launch_bounds__(64 * S::waves, 2) mx_proj_kernel(MxArgs p) {
 // its 128 columns of W in registers, all of K, and goes down the rows of A, 64 at a
 // time; two waves do all the loading, a tile each in turn, and the four that multiply
 // and store wait for nothing but their barrier.  Two workgroups a CU, out of step.
+// 76800 x 4096 x 640: 194 us back to back, 1.26 GB of output at 6.5 TB/s (a fill of that
+// size: 6.9); the same without its stores 85.
 // 64 rows x 128 columns, 32 x 64 a wave: it stores 256 bytes of a row at once (204 us
 // for 76800 x 4096 x 640, 230 in 128 bytes).  From 6 steps of 128 along K on, W's
 // registers allow 32 columns a wave only.
