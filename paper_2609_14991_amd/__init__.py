@@ -563,7 +563,9 @@ def quantize(x, stream=None):
     packed elements [R, K // 2] and scale bytes [R, mx_scale_stride(K)], both uint8."""
     import torch
 
-    _, R, K, stride = _rows(x.unsqueeze(0) if x.dim() == 2 else x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: rows [R, K] are wanted")
+    _, R, K, stride = _rows(x.unsqueeze(0), "x")
     q = torch.empty((R, K // 2), dtype=torch.uint8, device=x.device)
     s = torch.empty((R, mx_scale_stride(K)), dtype=torch.uint8, device=x.device)
     mx_quantize(x, stride, R, K, q, s, stream)

@@ -24,15 +24,12 @@ __device__ int32_t g_joint_score_status;
 // all of them.  Four operations a logit, the exponential among them; the maxima are
 // counted as one, which the sum less 1 then holds to 1e-5 unless next to nothing
 // else is in it.  Where that is so (one logit far above the row's others) or a
-// logit is -infinity (0 times it is NaN), once more with care.
+// logit is -infinity (0 times it leaves u NaN), once more with care.
 template <int TN>
 __device__ __forceinline__ Stat tile_row_stat(const f32x4 (&x)[TN]) {
-  float top = x[0][0], low = x[0][0];
+  float top = x[0][0];
 #pragma unroll
-  for (int j = 0; j < 4 * TN; ++j) {
-    top = fmaxf(top, x[j / 4][j % 4]);
-    low = fminf(low, x[j / 4][j % 4]);
-  }
+  for (int j = 1; j < 4 * TN; ++j) top = fmaxf(top, x[j / 4][j % 4]);
   Stat s{across_rows(top, [](float a, float b) { return fmaxf(a, b); }), 1.0f, 0.0f, 0.0f};
   const float shift = -s.m * kLog2e;
   float sum = 0.0f;
@@ -45,7 +42,7 @@ __device__ __forceinline__ Stat tile_row_stat(const f32x4 (&x)[TN]) {
   const auto add = [](float a, float b) { return a + b; };
   s.rest = across_rows(sum, add) - 1.0f;
   s.u = across_rows(s.u * kLn2, add);
-  if (__ballot(low == -INFINITY || s.rest < 0.0625f)) {
+  if (__ballot(s.u != s.u || s.rest < 0.0625f)) {
     float v[4 * TN];
 #pragma unroll
     for (int j = 0; j < 4 * TN; ++j) v[j] = x[j / 4][j % 4];
@@ -82,19 +79,20 @@ __global__ void __launch_bounds__(64 * S::waves, 2) joint_stat_kernel(StatArgs p
   // the sums start at the bias, at -infinity in columns past N: lane l holds row
   // l % 16 of each 16 x 16 tile, columns 4 * (l / 16) .. + 3
   f32x4 acc[S::TM][S::TN];
-#pragma unroll
-  for (int j = 0; j < S::TN; ++j) {
-    f32x4 b;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = bn + wn + j * 16 + fc * 4 + r;
-      b[r] = n >= p.N ? -INFINITY : p.bias ? p.bias[n] : 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < S::TM; ++i) acc[i][j] = b;
-  }
   Bf16Op op;
-  tile_product<S>(op, smem, p.A, p.W, p.M, p.N, p.K * 2, bm, bn, acc);
+  tile_product<S>(op, smem, p.A, p.W, p.M, p.N, p.K * 2, bm, bn, acc, [&](auto &c) {
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      f32x4 b;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int n = bn + wn + j * 16 + fc * 4 + r;
+        b[r] = n >= p.N ? -INFINITY : p.bias ? p.bias[n] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) c[i][j] = b;
+    }
+  });
 
   wait_barrier<0>();  // every wave has read the last stage
   f32x4 *stat = reinterpret_cast<f32x4 *>(smem);
@@ -106,12 +104,13 @@ __global__ void __launch_bounds__(64 * S::waves, 2) joint_stat_kernel(StatArgs p
   __syncthreads();
   for (int row = threadIdx.x; row < S::BM; row += 64 * S::waves) {
     if (bm + row >= p.M) break;
-    Stat s = stat_none();
+    Stat v[S::WN];
 #pragma unroll
     for (int q = 0; q < S::WN; ++q) {
-      const f32x4 v = stat[row * S::WN + q];
-      stat_join(s, Stat{v[0], v[1], v[2], v[3]});
+      const f32x4 w = stat[row * S::WN + q];
+      v[q] = Stat{w[0], w[1], w[2], w[3]};
     }
+    const Stat s = stat_of(v);
     float *o = p.part + (int64_t)tc * 4 * p.M + bm + row;
     o[0] = s.m;
     o[p.M] = s.ones;

@@ -28,9 +28,8 @@ __global__ void __launch_bounds__(64 * S::waves, 2) joint_proj_kernel(const uint
   int tr, tc;
   tile_place(map, n_col_tiles, tr, tc);
   f32x4 acc[S::TM][S::TN];
-  tile_zero<S>(acc);
   Bf16Op op;
-  tile_product<S>(op, smem, A, W, M, N, K * 2, tr * S::BM, tc * S::BN, acc);
+  tile_product<S>(op, smem, A, W, M, N, K * 2, tr * S::BM, tc * S::BN, acc, [](auto &c) { tile_zero<S>(c); });
   tile_store<S, kAux>(smem, bias, M, N, tr * S::BM, tc * S::BN, acc, out);
 }
 

@@ -195,10 +195,11 @@ __device__ __forceinline__ void tile_stage(const Op &op, const unsigned char *pa
   step(std::integral_constant<int, 1>{});
 }
 
-// adds the tile at row bm, column bn to acc
-template <class S, class Op>
+// The tile at row bm, column bn, added to what `start` puts into acc while the first
+// stages are on their way
+template <class S, class Op, class Start>
 __device__ __forceinline__ void tile_product(Op &op, unsigned char *smem, const void *A, const void *W, int M, int N,
-                                             int row_bytes, int bm, int bn, f32x4 (&acc)[S::TM][S::TN]) {
+                                             int row_bytes, int bm, int bn, f32x4 (&acc)[S::TM][S::TN], Start start) {
   TileLoads<S> loads(A, W, M, N, row_bytes);
   constexpr int kL = TileLoads<S>::kL;
   const int lane = threadIdx.x & 63, wave = loads.wave;
@@ -209,6 +210,7 @@ __device__ __forceinline__ void tile_product(Op &op, unsigned char *smem, const 
 #pragma unroll
   for (int s = 0; s < S::NB - 1; ++s)
     if (s < nk) loads.issue(s, smem + s * S::stage);
+  start(acc);
   int buf = 0;
   for (int s = 0; s < nk; ++s) {
     // stage s has landed for every wave, and every wave is done reading the

@@ -168,13 +168,12 @@ __global__ void __launch_bounds__(64 * S::waves, 2) mx_proj_kernel(MxArgs p) {
   int tr, tc;
   tile_place(p.map, p.n_col_tiles, tr, tc);
   f32x4 acc[S::TM][S::TN];
-  tile_zero<S>(acc);
   MxOp<S::TM, S::TN> op;
   op.A_scales = p.A_scales;
   op.W_scales = p.W_scales;
   op.blocks = p.K / kBlock;
   op.stride = FUSION_MX_SCALE_STRIDE(p.K);
-  tile_product<S>(op, smem, p.A, p.W, p.M, p.N, p.K / 2, tr * S::BM, tc * S::BN, acc);
+  tile_product<S>(op, smem, p.A, p.W, p.M, p.N, p.K / 2, tr * S::BM, tc * S::BN, acc, [](auto &c) { tile_zero<S>(c); });
   tile_store<S, kAux>(smem, p.bias, p.M, p.N, tr * S::BM, tc * S::BN, acc, p.out);
 }
 

@@ -162,6 +162,24 @@ __device__ __forceinline__ void stat_join(Stat &s, Stat o) {
   s.u += o.u;
 }
 
+// several sets' statistics as one
+template <int n>
+__device__ __forceinline__ Stat stat_of(const Stat (&v)[n]) {
+  Stat s = stat_none();
+#pragma unroll
+  for (int q = 0; q < n; ++q) s.m = fmaxf(s.m, v[q].m);
+  const float base = s.m == -INFINITY ? 0.0f : s.m;
+#pragma unroll
+  for (int q = 0; q < n; ++q) {
+    const float d = fmaxf(v[q].m - base, kFar), f = exp_of(d), all = v[q].ones + v[q].rest;
+    const bool top = v[q].m == s.m;
+    s.ones += top ? v[q].ones : 0.0f;
+    s.rest += top ? v[q].rest : f * all;
+    s.u += f * (v[q].u + d * all);
+  }
+  return s;
+}
+
 // the 64 lanes' statistics as one, in every lane
 __device__ __forceinline__ void stat_wave(Stat &s) {
   stat_lift(s, wave_max(s.m));

@@ -382,7 +382,7 @@ def test_conveniences_refuse_what_the_calls_would_misread():
     """CPU tensors, other types, other shapes and orders: refused before anything is launched."""
     x, tok = torch.zeros((2, 4, 8)), torch.zeros((2, 4), dtype=torch.int32)
     for call in (lambda: F.score(x, tok), lambda: F.score_projected(x.bfloat16(), torch.zeros((8, 8), dtype=torch.bfloat16)),
-                 lambda: F.quantize(torch.zeros((4, 32))), lambda: F.dequantize(torch.zeros((4, 16), dtype=torch.uint8), torch.zeros((4, 8), dtype=torch.uint8)),
+                 lambda: F.quantize(torch.zeros((4, 32))), lambda: F.quantize(torch.zeros((2, 4, 32))), lambda: F.dequantize(torch.zeros((4, 16), dtype=torch.uint8), torch.zeros((4, 8), dtype=torch.uint8)),
                  lambda: F.score_backward(x, dict(logp=None, entropy=None, lse=None), tok, None, 1, torch.zeros((2, 4)))):
         with pytest.raises(ValueError):
             call()
