@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "fusion_internal.h"
 #include "row_types.h"
@@ -229,7 +230,8 @@ struct ScoreArgs {
 // 74 % of the time on the beam above, 87 % on 16000 x 8190 in bf16).
 // (32 values a lane instead of 16: half the waves fit, 173 -> 204 us for 76800 rows
 // of 4096 in bf16 with 4 alternatives.)
-template <class T, int W>
+// beam: there are parents.
+template <class T, int W, bool beam>
 __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs p) {
   constexpr int kWaves = W == 1 ? 4 : W;
   __shared__ int s_val[kWaves][kList];
@@ -243,28 +245,31 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs 
   const float nan = __int_as_float(0x7FC00000);
 
   // The tokens chosen on this row: lane i looks at slot i of the row's stream
-  const int slots = p.parents ? p.B : 1, first = p.parents ? r / p.B * p.B : r, m = first + lane;
+  const int slots = beam ? p.B : 1, first = beam ? r / p.B * p.B : r, m = first + lane;
   const T *row = static_cast<const T *>(p.logits) + r * p.stride;
   int par = lane, tok = -1;
   if (lane < slots) {
-    if (p.parents) par = p.parents[m];
+    if (beam) par = p.parents[m];
     if (p.tokens) tok = p.tokens[m];
   }
-  const bool bad_token = tok < -1 || tok >= p.V, bad_parent = par < -1 || par >= slots;
-  const bool mine = lane < slots && (p.parents ? par == r - first : true);
-  const unsigned long long any = __ballot(mine);
-  if (p.parents && wave % W == 0 && lane == r - first && (par == -1 || bad_parent)) {
-    // the slot of the row's own number is dead: nobody else writes its outputs
-    if (p.logp) p.logp[r] = bad_token || bad_parent ? nan : 0.0f;
-    if (p.entropy) p.entropy[r] = bad_parent ? nan : 0.0f;
-    if (p.lse) p.lse[r] = bad_parent ? nan : -INFINITY;
-    for (int j = 0; j < p.k; ++j) {
-      p.top_tokens[(int64_t)r * p.k + j] = -1;
-      p.top_logp[(int64_t)r * p.k + j] = bad_parent ? nan : -INFINITY;
+  const bool bad_token = tok < -1 || tok >= p.V;
+  const bool mine = lane < slots && (!beam || par == r - first);
+  const unsigned long long any = beam ? __ballot(mine) : 1;
+  if (beam) {
+    const bool bad_parent = par < -1 || par >= slots;
+    if (wave % W == 0 && lane == r - first && (par == -1 || bad_parent)) {
+      // the slot of the row's own number is dead: nobody else writes its outputs
+      if (p.logp) p.logp[r] = bad_token || bad_parent ? nan : 0.0f;
+      if (p.entropy) p.entropy[r] = bad_parent ? nan : 0.0f;
+      if (p.lse) p.lse[r] = bad_parent ? nan : -INFINITY;
+      for (int j = 0; j < p.k; ++j) {
+        p.top_tokens[(int64_t)r * p.k + j] = -1;
+        p.top_logp[(int64_t)r * p.k + j] = bad_parent ? nan : -INFINITY;
+      }
+      if (bad_token || bad_parent) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
     }
-    if (bad_token || bad_parent) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);
+    if (!any) return;  // (the same in every wave of the row)
   }
-  if (!any) return;  // (the same in every wave of the row)
   float x_tok = 0.0f;
   if (mine && wave % W == 0 && tok >= 0 && !bad_token) x_tok = to_float(row[tok]);
   WaveStat ws = wave_stat_none();
@@ -316,7 +321,7 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) score_kernel(ScoreArgs 
     const int top = q.bad ? -1 : id;
     const float top_logp = q.bad ? nan : id < 0 ? -INFINITY : row_logp(q, of_order(v));
     for (unsigned long long todo = any; todo; todo &= todo - 1) {
-      const int64_t at = (int64_t)(first + __builtin_ctzll(todo)) * p.k + lane;
+      const int64_t at = (int64_t)(first + (beam ? __builtin_ctzll(todo) : 0)) * p.k + lane;
       if (lane < p.k) {
         p.top_tokens[at] = top;
         p.top_logp[at] = top_logp;
@@ -514,8 +519,9 @@ extern "C" int token_logprobs(const void *logits, int32_t dtype, int64_t stride,
   if (!logp && !entropy && !lse && k == 0) return set_error(FUSION_E_ARG, "no output buffer");
   const ScoreArgs p{logits, logp ? tokens : nullptr, parents, logp, entropy, lse, top_logp, top_tokens, stride, (int32_t)M,
                     B, V, k};
-  auto go = [&](auto type) {
+  auto launch = [&](auto type, auto beam_) {
     using T_ = decltype(type);
+    constexpr bool beam = decltype(beam_)::value;
     // Waves a row, enough rows or chunks to fill the chip (us; fp32, 4 alternatives):
     //                 1      4      8      16
     //    6000 x 2500  17.4   27.2                 (a wave alone joins nothing)
@@ -526,14 +532,15 @@ extern "C" int token_logprobs(const void *logits, int32_t dtype, int64_t stride,
     //    300 x 32000         19.9   15.4   18.0
     //    513 x 100003        54     40     50     (bf16)
     if (M >= 4096 || (M >= 2048 && V <= 4 * kChunk) || V <= kChunk)
-      hipLaunchKernelGGL((score_kernel<T_, 1>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, stream, p);
+      hipLaunchKernelGGL((score_kernel<T_, 1, beam>), dim3((unsigned)((M + 3) / 4)), dim3(256), 0, stream, p);
     else if (M >= 1024 || V <= 4 * kChunk)
-      hipLaunchKernelGGL((score_kernel<T_, 4>), dim3((unsigned)M), dim3(256), 0, stream, p);
+      hipLaunchKernelGGL((score_kernel<T_, 4, beam>), dim3((unsigned)M), dim3(256), 0, stream, p);
     else if (M >= 256 || V <= 8 * kChunk)
-      hipLaunchKernelGGL((score_kernel<T_, 8>), dim3((unsigned)M), dim3(512), 0, stream, p);
+      hipLaunchKernelGGL((score_kernel<T_, 8, beam>), dim3((unsigned)M), dim3(512), 0, stream, p);
     else
-      hipLaunchKernelGGL((score_kernel<T_, 16>), dim3((unsigned)M), dim3(1024), 0, stream, p);
+      hipLaunchKernelGGL((score_kernel<T_, 16, beam>), dim3((unsigned)M), dim3(1024), 0, stream, p);
   };
+  auto go = [&](auto type) { parents ? launch(type, std::true_type{}) : launch(type, std::false_type{}); };
   if (dtype == FUSION_F32) go(float{});
   else if (dtype == FUSION_BF16) go(Brain{});
   else go(Half{});
