@@ -380,12 +380,27 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+_current = None
+
+
+def _on(stream):
+    """``_stream`` as a plain int, torch's functions looked up once."""
+    global _current
+    if stream is not None:
+        return int(stream)
+    if _current is None:
+        import torch
+
+        _current = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+    return _current[0](_current[1]())
+
+
 def token_logprobs(logits, stride, T, S, B, V, tokens, parents, k, logp, entropy, lse, top_tokens=None, top_logp=None,
                    stream=None):
     """Same arguments as the C call, the dtype taken from logits; CUDA (HIP) tensors, float32 outputs."""
     _check(lib().token_logprobs(_at(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V), _at(tokens),
                                 _at(parents), int(k), _at(logp), _at(entropy), _at(lse), _at(top_tokens),
-                                _at(top_logp), _stream(stream)))
+                                _at(top_logp), _on(stream)))
 
 
 def token_logprobs_backward(logits, stride, T, S, B, V, tokens, parents, logp, entropy, lse, grad_logp, grad_entropy,
@@ -396,7 +411,7 @@ def token_logprobs_backward(logits, stride, T, S, B, V, tokens, parents, logp, e
     _check(lib().token_logprobs_backward(_at(logits), _dtype(logits), int(stride), int(T), int(S), int(B), int(V),
                                          _at(tokens), _at(parents), _at(logp), _at(entropy), _at(lse),
                                          _at(grad_logp), _at(grad_entropy), _at(grad_logits), int(grad_stride),
-                                         _stream(stream)))
+                                         _on(stream)))
 
 
 def joint_logprobs_workspace(M, V, K) -> int:
@@ -410,7 +425,7 @@ def joint_logprobs(A, W, bias, K, T, S, B, V, tokens, parents, logp, entropy, ls
     """Same arguments as the C call (the workspace's size is its tensor's); A and W bfloat16 (or int16 bit patterns)."""
     _check(lib().joint_logprobs(_at(A), _at(W), _at(bias), int(K), int(T), int(S), int(B), int(V), _at(tokens),
                                 _at(parents), _at(logp), _at(entropy), _at(lse), _at(workspace),
-                                workspace.numel(), _stream(stream)))
+                                workspace.numel(), _on(stream)))
 
 
 def mx_scale_stride(K) -> int:
@@ -420,19 +435,19 @@ def mx_scale_stride(K) -> int:
 
 def mx_quantize(x, stride, R, K, q, scales, stream=None):
     """Same arguments as the C call, the dtype taken from x; q [R, K // 2] and scales [R, mx_scale_stride(K)] uint8."""
-    _check(lib().mx_quantize(_at(x), _dtype(x), int(stride), int(R), int(K), _at(q), _at(scales), _stream(stream)))
+    _check(lib().mx_quantize(_at(x), _dtype(x), int(stride), int(R), int(K), _at(q), _at(scales), _on(stream)))
 
 
 def mx_dequantize(q, scales, R, K, out, stride, stream=None):
     """Same arguments as the C call, the dtype taken from out."""
     _check(lib().mx_dequantize(_at(q), _at(scales), int(R), int(K), _at(out), _dtype(out), int(stride),
-                               _stream(stream)))
+                               _on(stream)))
 
 
 def joint_project_mx(A, A_scales, W, W_scales, bias, M, N, K, out, stream=None):
     """Same arguments as the C call; operands as mx_quantize writes them, bias and out float32 CUDA tensors."""
     _check(lib().joint_project_mx(_at(A), _at(A_scales), _at(W), _at(W_scales), _at(bias), int(M), int(N), int(K),
-                                  _at(out), _stream(stream)))
+                                  _at(out), _on(stream)))
 
 
 def fusion_device_status(stream=None) -> int:
