@@ -17,6 +17,7 @@
 #include <cstring>
 
 #include "fusion_internal.h"
+#include "score_status.h"
 
 namespace fusion {
 namespace {
@@ -77,14 +78,20 @@ __device__ int32_t g_end_status;
 
 }  // namespace
 
-// the status bits of the end-of-stream kernel, cleared (fusion_device_status
-// merges them with the fusion kernels' own)
+// the status bits of the end-of-stream kernel and of the scoring kernels, cleared
+// (fusion_device_status merges them with the fusion kernels' own)
 int end_status_take(int32_t *bits) {
   int32_t v = 0, zero = 0;
   hipError_t e = hipMemcpyFromSymbol(&v, HIP_SYMBOL(g_end_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
   if (e != hipSuccess) return hip_error(e, "hipMemcpyFromSymbol");
   e = hipMemcpyToSymbol(HIP_SYMBOL(g_end_status), &zero, sizeof(int32_t), 0, hipMemcpyHostToDevice);
   if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
+  for (auto take : {score_status_take, joint_score_status_take}) {
+    int32_t more = 0;
+    const int rc = take(&more);
+    if (rc != FUSION_OK) return rc;
+    v |= more;
+  }
   *bits = v;
   return FUSION_OK;
 }

@@ -93,7 +93,4 @@ int set_error(int code, const std::string &msg);
 int hip_error(hipError_t e, const char *what);
 // status bits of the end-of-stream kernel, taken and cleared (end_scores.hip)
 int end_status_take(int32_t *bits);
-// the same of the scoring kernels (logprobs.hip, joint_logprobs.hip)
-int score_status_take(int32_t *bits);
-int joint_score_status_take(int32_t *bits);
 }  // namespace fusion

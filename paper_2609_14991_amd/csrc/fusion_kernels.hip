@@ -404,13 +404,10 @@ extern "C" int fusion_device_status(hipStream_t stream, int32_t *code) {
   int zero = 0;
   e = hipMemcpyToSymbol(HIP_SYMBOL(g_status), &zero, sizeof(int), 0, hipMemcpyHostToDevice);
   if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
-  for (auto take : {end_status_take, score_status_take, joint_score_status_take}) {
-    int32_t bits = 0;
-    const int rc = take(&bits);
-    if (rc != FUSION_OK) return rc;
-    v |= bits;
-  }
-  *code = v;
+  int32_t end_bits = 0;
+  const int rc = end_status_take(&end_bits);
+  if (rc != FUSION_OK) return rc;
+  *code = v | end_bits;
   return FUSION_OK;
 }
 

@@ -13,6 +13,7 @@
 
 #include "fusion_internal.h"
 #include "joint_tile.h"
+#include "score_status.h"
 #include "wave_ops.h"
 
 namespace fusion {
@@ -60,8 +61,8 @@ struct StatArgs {
   int M, N, K, n_col_tiles, map;
 };
 
-// A workgroup a tile, as joint_proj_kernel.  76800 x 4096 x 640: 385 us back to back
-// (1.05 PFLOP/s; the logits' projection alone, with its stores, 456), of which the
+// A workgroup a tile, as joint_proj_kernel.  76800 x 4096 x 640: 377 us back to back
+// (1.07 PFLOP/s; the logits' projection alone, with its stores, 456), of which the
 // products take 290 and the statistics behind them the rest: with 128 KB of stages a
 // CU holds one workgroup, and nothing runs beside its vector work.  What would overlap
 // the two was slower: workgroups that go on from tile to tile with the next one's stages

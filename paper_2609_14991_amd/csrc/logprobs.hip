@@ -16,6 +16,7 @@
 
 #include "fusion_internal.h"
 #include "row_types.h"
+#include "score_status.h"
 #include "wave_ops.h"
 
 namespace fusion {
@@ -470,7 +471,7 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
 
 }  // namespace
 
-// the status bits of the scoring kernels, cleared (fusion_device_status merges them)
+// the status bits of the kernels above, cleared
 int score_status_take(int32_t *bits) {
   int32_t v = 0, zero = 0;
   hipError_t e = hipMemcpyFromSymbol(&v, HIP_SYMBOL(g_score_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
