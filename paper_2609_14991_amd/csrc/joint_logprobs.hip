@@ -24,8 +24,9 @@ __device__ int32_t g_joint_score_status;
 // Statistics of a row's 16 TN logits in four lanes (l, l ^ 16, l ^ 32, l ^ 48), in
 // all of them.  Four operations a logit, the exponential among them; the maxima are
 // counted as one, which the sum less 1 then holds to 1e-5 unless next to nothing
-// else is in it.  Where that is so (one logit far above the row's others) or a
-// logit is -infinity (0 times it leaves u NaN), once more with care.
+// else is in it.  Where that is so (one logit far above the row's others), a logit is
+// -infinity (0 times it leaves u NaN) or the largest is near the type's lowest value
+// (its product with log2 e overflows), once more with care.
 template <int TN>
 __device__ __forceinline__ Stat tile_row_stat(const f32x4 (&x)[TN]) {
   float top = x[0][0];
@@ -43,7 +44,7 @@ __device__ __forceinline__ Stat tile_row_stat(const f32x4 (&x)[TN]) {
   const auto add = [](float a, float b) { return a + b; };
   s.rest = across_rows(sum, add) - 1.0f;
   s.u = across_rows(s.u * kLn2, add);
-  if (__ballot(s.u != s.u || s.rest < 0.0625f)) {
+  if (__ballot(s.u != s.u || !(s.rest >= 0.0625f && s.rest < INFINITY))) {
     float v[4 * TN];
 #pragma unroll
     for (int j = 0; j < 4 * TN; ++j) v[j] = x[j / 4][j % 4];

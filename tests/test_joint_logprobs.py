@@ -178,6 +178,27 @@ def test_masked_tokens(V):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V", [40, 700, 4100])
+@pytest.mark.parametrize("low", [float(np.finfo(np.float32).min), -3e38, -1e30])
+def test_tokens_masked_by_a_low_value(V, low):
+    """As torch.finfo(...).min masks: single tokens, runs that fill whole tiles of columns, the whole vocabulary."""
+    rng = np.random.default_rng(V)
+    M, K = 40, 72
+    A, W, bias = _joint(rng, M, V, K)
+    tok = rng.integers(0, V, (1, M))
+    for masked in (rng.random(V) < 0.3, np.arange(V) >= V // 4, np.arange(V) < V - 3, np.ones(V, dtype=bool)):
+        b = np.where(masked, np.float32(low), bias).astype(np.float32)
+        got = _run(A, W, b, 1, M, 1, tok, None)
+        # in fp32 a masked logit is the mask: the product is far below its last place
+        x = np.where(masked, float(np.float32(low)), projection.joint_project(A, W, np.where(masked, 0, b)))[None]
+        ref = O.scores(x, tok, None, M, 1, 0)
+        d = projection.fp32_error_bound(A, W, np.where(masked, 0, b)).max()
+        for n in ("logp", "lse", "entropy"):
+            tol = 2 * ref["tol_" + n] + 1e-5 + 16 * d
+            assert np.all(np.abs(got[n] - ref[n]) <= tol), (n, int(masked.sum()))
+
+
+@pytest.mark.gpu
 def test_confident_rows_from_hidden_states():
     """One token far above the rest: -log p is the rest's sum, whose terms' differences the logits' errors bound."""
     rng = np.random.default_rng(14)
