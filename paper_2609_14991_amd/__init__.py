@@ -11,6 +11,7 @@ fallback.
 from __future__ import annotations
 
 import atexit
+import contextlib
 import ctypes
 import os
 import sys
@@ -395,6 +396,16 @@ def _on(stream):
     return _current[0](_current[1]())
 
 
+def _made_for(stream):
+    """Tensors made inside are made on ``stream`` (an address; None: the current stream): their memory goes from one
+    use on that stream to the next one there, and not to the current stream's work while ``stream`` still uses it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream)))
+
+
 def token_logprobs(logits, stride, T, S, B, V, tokens, parents, k, logp, entropy, lse, top_tokens=None, top_logp=None,
                    stream=None):
     """Same arguments as the C call, the dtype taken from logits; CUDA (HIP) tensors, float32 outputs."""
@@ -458,6 +469,10 @@ def fusion_device_status(stream=None) -> int:
 
 # ---------------------------------------------------------------------------
 # conveniences that allocate the outputs with torch (still no compute here)
+#
+# ``stream`` is the address of the stream to work on.  What score, score_backward, score_projected, quantize,
+# dequantize and project_mx return was made on it, as a tensor of ``with torch.cuda.stream(...)``: another
+# stream that uses it waits for this one and calls record_stream.
 # ---------------------------------------------------------------------------
 def step(lm, trie, logits, lm_state, boost_state, lam, beta, blank_id, k, blank_mode,
          want_fused=False, stream=None):
@@ -521,8 +536,9 @@ def score(logits, tokens=None, parents=None, B=1, k=0, stream=None):
         if t is not None:
             _want(t, what, torch.int32, (T, H))
     new = lambda dt, *n: torch.empty((T, H) + n, dtype=dt, device=logits.device)  # noqa: E731
-    out = dict(logp=None if tokens is None else new(torch.float32), entropy=new(torch.float32), lse=new(torch.float32),
-               top=new(torch.int32, k) if k else None, top_logp=new(torch.float32, k) if k else None)
+    with _made_for(stream):
+        out = dict(logp=None if tokens is None else new(torch.float32), entropy=new(torch.float32), lse=new(torch.float32),
+                   top=new(torch.int32, k) if k else None, top_logp=new(torch.float32, k) if k else None)
     token_logprobs(logits, stride, T, H // B, B, V, tokens, parents, k, out["logp"], out["entropy"], out["lse"], out["top"],
                    out["top_logp"], stream)
     return out
@@ -544,7 +560,8 @@ def score_backward(logits, scored, tokens=None, parents=None, B=1, grad_logp=Non
     for n in ("logp", "entropy", "lse"):
         if scored[n] is not None:
             _want(scored[n], n, torch.float32, (T, H))
-    grad = logits if in_place else torch.empty((T, H, V), dtype=logits.dtype, device=logits.device)
+    with _made_for(stream):
+        grad = logits if in_place else torch.empty((T, H, V), dtype=logits.dtype, device=logits.device)
     token_logprobs_backward(logits, stride, T, H // B, B, V, tokens, parents, scored["logp"], scored["entropy"], scored["lse"],
                             grad_logp, grad_entropy, grad, stride if in_place else V, stream)
     return grad
@@ -567,8 +584,9 @@ def score_projected(A, W, bias=None, tokens=None, parents=None, B=1, stream=None
         if t is not None:
             _want(t, what, torch.int32, (T, H))
     new = lambda: torch.empty((T, H), dtype=torch.float32, device=A.device)  # noqa: E731
-    out = dict(logp=None if tokens is None else new(), entropy=new(), lse=new())
-    work = torch.empty(joint_logprobs_workspace(T * H, V, K), dtype=torch.float32, device=A.device)
+    with _made_for(stream):
+        out = dict(logp=None if tokens is None else new(), entropy=new(), lse=new())
+        work = torch.empty(joint_logprobs_workspace(T * H, V, K), dtype=torch.float32, device=A.device)
     joint_logprobs(A, W, bias, K, T, H // B, B, V, tokens, parents, out["logp"], out["entropy"], out["lse"], work, stream)
     return out
 
@@ -581,8 +599,9 @@ def quantize(x, stream=None):
     if x.dim() != 2:
         raise ValueError("x: rows [R, K] are wanted")
     _, R, K, stride = _rows(x.unsqueeze(0), "x")
-    q = torch.empty((R, K // 2), dtype=torch.uint8, device=x.device)
-    s = torch.empty((R, mx_scale_stride(K)), dtype=torch.uint8, device=x.device)
+    with _made_for(stream):
+        q = torch.empty((R, K // 2), dtype=torch.uint8, device=x.device)
+        s = torch.empty((R, mx_scale_stride(K)), dtype=torch.uint8, device=x.device)
     mx_quantize(x, stride, R, K, q, s, stream)
     return q, s
 
@@ -594,7 +613,8 @@ def dequantize(q, scales, dtype=None, stream=None):
     R, K = q.shape[0], 2 * q.shape[1]
     _want(q, "q", torch.uint8, (R, K // 2))
     _want(scales, "scales", torch.uint8, (R, mx_scale_stride(K)))
-    out = torch.empty((R, K), dtype=torch.float32 if dtype is None else dtype, device=q.device)
+    with _made_for(stream):
+        out = torch.empty((R, K), dtype=torch.float32 if dtype is None else dtype, device=q.device)
     mx_dequantize(q, scales, R, K, out, K, stream)
     return out
 
@@ -611,7 +631,8 @@ def project_mx(A, W, bias=None, stream=None):
         _want(t, what, torch.uint8, shape)
     if bias is not None:
         _want(bias, "bias", torch.float32, (N,))
-    out = torch.empty((M, N), dtype=torch.float32, device=qa.device)
+    with _made_for(stream):
+        out = torch.empty((M, N), dtype=torch.float32, device=qa.device)
     joint_project_mx(qa, sa, qw, sw, bias, M, N, K, out, stream)
     return out
 
