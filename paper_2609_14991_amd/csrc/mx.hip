@@ -228,7 +228,8 @@ __global__ void __launch_bounds__(64 * 6, 3) mx_panel_kernel(PanelArgs q) {
   if (wave >= S::waves) {
     const int who = wave - S::waves;
     const __amdgpu_buffer_rsrc_t ra = rsrc(p.A, (uint32_t)((int64_t)p.M * (p.K / 2)));
-    const __amdgpu_buffer_rsrc_t rs = rsrc(p.A_scales, (uint32_t)((int64_t)p.M * stride));
+    const uint32_t scale_bytes = (uint32_t)((int64_t)p.M * stride);
+    const __amdgpu_buffer_rsrc_t rs = rsrc(p.A_scales, scale_bytes);
     // a load brings 16 rows of a step, 4 chunks each; lane l's lands in row l / 4, slot l % 4
     const int row = lane >> 2, chunk = Slots64::of(row, lane & 3);
     auto issue = [&](int k) {
@@ -245,12 +246,13 @@ __global__ void __launch_bounds__(64 * 6, 3) mx_panel_kernel(PanelArgs q) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
           load_lds(ra, at + (s * 4 + j) * 1024, s < steps - 1 || s * 4 + chunk < blocks ? vo[j] : kOutside, s * 64);
-      // the scales of 64 rows lie together: 256 bytes a load (past the operand: zeros)
+      // the scales of 64 rows lie together: 256 bytes a load, zeros past the operand (the
+      // whole distance in the lane's offset: a scalar one is not range checked)
       const uint32_t so = (uint32_t)((int64_t)tile * S::BM * stride + lane * 4);
 #pragma unroll
       for (int j = 0; j < stride / 4; ++j)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(at + kScales + j * 256), 4, so,
-                                                 j * 256, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void *)(at + kScales + j * 256), 4,
+                                                 so + j * 256 < scale_bytes ? so + j * 256 : kOutside, 0, 0, 0);
     };
     // the workgroup's tiles `who`, `who` + 2 ..: each into this wave's buffer, once
     // the others are behind the barrier of the tile after the one that was there
