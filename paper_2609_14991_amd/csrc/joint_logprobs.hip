@@ -22,18 +22,20 @@ namespace {
 __device__ int32_t g_joint_score_status;
 
 // Statistics of a row's 16 TN logits in four lanes (l, l ^ 16, l ^ 32, l ^ 48), in
-// all of them.  Four operations a logit, the exponential among them; the maxima are
-// counted as one, which the sum less 1 then holds to 1e-5 unless next to nothing
-// else is in it.  Where that is so (one logit far above the row's others), a logit is
-// -infinity (0 times it leaves u NaN) or the largest is near the type's lowest value
-// (its product with log2 e overflows), once more with care.
+// all of them.  Four operations a logit, the exponential among them: (x - m) log2 e is
+// one fma of x, off by what the rounding of m log2 e left, the same for the whole row,
+// and the sums are put right by it.  The maxima are counted as one, the sum less 1: the
+// sum's roundings (24 halves of a last place at most) are 2.4e-5 or less of a rest of 1/16
+// or more, whatever m is.  Where the rest is less (one logit far above the row's others),
+// a logit is -infinity (0 times it leaves u NaN) or the largest is past 2800 (the
+// shift past 4096, its rounding past 2^-12), once more with care.
 template <int TN>
 __device__ __forceinline__ Stat tile_row_stat(const f32x4 (&x)[TN]) {
   float top = x[0][0];
 #pragma unroll
   for (int j = 1; j < 4 * TN; ++j) top = fmaxf(top, x[j / 4][j % 4]);
   Stat s{across_rows(top, [](float a, float b) { return fmaxf(a, b); }), 1.0f, 0.0f, 0.0f};
-  const float shift = -s.m * kLog2e;
+  const float shift = -s.m * kLog2e, off = fmaf(-s.m, kLog2e, -shift);
   float sum = 0.0f;
 #pragma unroll
   for (int j = 0; j < 4 * TN; ++j) {
@@ -42,9 +44,11 @@ __device__ __forceinline__ Stat tile_row_stat(const f32x4 (&x)[TN]) {
     s.u = fmaf(t, e, s.u);
   }
   const auto add = [](float a, float b) { return a + b; };
-  s.rest = across_rows(sum, add) - 1.0f;
-  s.u = across_rows(s.u * kLn2, add);
-  if (__ballot(s.u != s.u || !(s.rest >= 0.0625f && s.rest < INFINITY))) {
+  sum = across_rows(sum, add);
+  const float by = fmaf(off, kLn2, 1.0f);  // 2^off, to 2^-25 for an |off| up to 2^-12
+  s.rest = fmaf(sum, by, -1.0f);
+  s.u = fmaf(off, sum, across_rows(s.u, add)) * (by * kLn2);
+  if (__ballot(s.u != s.u || !(s.rest >= 0.0625f && fabsf(shift) < 4096.0f))) {
     float v[4 * TN];
 #pragma unroll
     for (int j = 0; j < 4 * TN; ++j) v[j] = x[j / 4][j % 4];
