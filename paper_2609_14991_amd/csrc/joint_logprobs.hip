@@ -82,8 +82,8 @@ __global__ void __launch_bounds__(64 * S::waves, 2) joint_stat_kernel(StatArgs p
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int fr = lane & 15, fc = lane >> 4;
   const int wm = (wave / S::WN) * S::RM, wn = (wave % S::WN) * S::RN;
-  // the sums start at the bias, at -infinity in columns past N: lane l holds row
-  // l % 16 of each 16 x 16 tile, columns 4 * (l / 16) .. + 3
+  // the sums start at the bias: lane l holds row l % 16 of each 16 x 16 tile, columns
+  // 4 * (l / 16) .. + 3
   f32x4 acc[S::TM][S::TN];
   Bf16Op op;
   tile_product<S>(op, smem, p.A, p.W, p.M, p.N, p.K * 2, bm, bn, acc, [&](auto &c) {
@@ -93,12 +93,25 @@ __global__ void __launch_bounds__(64 * S::waves, 2) joint_stat_kernel(StatArgs p
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int n = bn + wn + j * 16 + fc * 4 + r;
-        b[r] = n >= p.N ? -INFINITY : p.bias ? p.bias[n] : 0.0f;
+        b[r] = p.bias && n < p.N ? p.bias[n] : 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < S::TM; ++i) c[i][j] = b;
     }
   });
+  // columns past N are -infinity (not from the start: their weights are zeros, and a
+  // state that is not finite times 0 would make them NaN)
+  if (bn + S::BN > p.N) {
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      if (bn + wn + j * 16 + 16 <= p.N) continue;  // uniform
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (bn + wn + j * 16 + fc * 4 + r >= p.N)
+#pragma unroll
+          for (int i = 0; i < S::TM; ++i) acc[i][j][r] = -INFINITY;
+    }
+  }
 
   wait_barrier<0>();  // every wave has read the last stage
   f32x4 *stat = reinterpret_cast<f32x4 *>(smem);

@@ -78,3 +78,27 @@ def test_equal_logits_are_uniform_at_every_magnitude(V, value):
     got = _run(np.zeros_like(A), W, np.full(V, value, dtype=np.float32), 1, 30, 1, rng.integers(0, V, (1, 30)), None)
     tol = (REST + 8 * O.U32) * np.log(V)
     assert np.all(np.abs(got["logp"] + np.log(V)) <= tol) and np.all(np.abs(got["entropy"] - np.log(V)) <= tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [1, 3, 40, 127, 129, 1000])
+def test_states_that_are_not_finite(V):
+    """Rows whose logits all overflow to -infinity, to both infinities or are NaN: as the scores of those logits,
+    whatever part of a column tile lies past the vocabulary."""
+    rng = np.random.default_rng(V)
+    M, K = 8, 64
+    A, W = _exact_joint(rng, M, V, K)
+    W[:, 5] = to_bf16_bits(np.full(V, -0.5, dtype=np.float32))   # state 5 lowers every logit
+    W[:, 6] = to_bf16_bits(np.where(np.arange(V) % 2, 0.5, -0.5).astype(np.float32))
+    A[1, 5] = to_bf16_bits(np.array([np.inf], dtype=np.float32))[0]
+    A[2, 5] = to_bf16_bits(np.array([-np.inf], dtype=np.float32))[0]
+    A[3, 6] = to_bf16_bits(np.array([np.inf], dtype=np.float32))[0]
+    A[4, 0] = 0x7FC0                                              # NaN
+    tok = rng.integers(0, V, (1, M))
+    got = _run(A, W, None, 1, M, 1, tok, None)
+    assert got["lse"][0, 1] == -np.inf and got["logp"][0, 1] == -np.inf and got["entropy"][0, 1] == 0
+    for r in (2, 4) + ((3,) if V > 1 else ()):
+        assert all(np.isnan(got[n][0, r]) for n in got)
+    if V == 1:
+        assert got["lse"][0, 3] == -np.inf
+    assert all(np.isfinite(got[n][0, [0, 5, 6, 7]]).all() for n in got)
