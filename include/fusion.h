@@ -392,10 +392,13 @@ int token_logprobs(const void *logits, int32_t dtype, int64_t stride, int32_t T,
  *                written whole: 0 for a row on which no token was chosen and for one of
  *                -inf alone, NaN for one with a NaN or +inf.  May be logits itself with
  *                the same stride; otherwise the two must not overlap
- * Sums are fp32 in a fixed order, rounded once to dtype; p is e^(x - lse) from the
- * rounded lse, but a token's own column comes from logp.  The alternatives have no
- * gradient.  A token out of range counts as none, a parent out of range as a dead
- * slot, and FUSION_STATUS_BAD_TOKEN is set.  Only enqueues work on `stream`; no workspace.
+ * Sums are fp32 in a fixed order, rounded once to dtype.  A token's own column comes
+ * from logp, and so does what the rounding of lse left out of p = e^(x - lse): with
+ * tokens and logp given, also where grad_logp is NULL, p is off by a few 2^-24 of log p of
+ * itself, and at most by half a last place of lse, as it is without them.  The
+ * alternatives have no gradient.  A token out of range counts as none, a parent out of
+ * range as a dead slot, and FUSION_STATUS_BAD_TOKEN is set.  Only enqueues work on
+ * `stream`; no workspace.
  */
 int token_logprobs_backward(const void *logits, int32_t dtype, int64_t stride, int32_t T, int32_t S, int32_t B,
                             int32_t V, const int32_t *tokens, const int32_t *parents, const float *logp,

@@ -373,11 +373,11 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
   float gl = 0.0f, ge = 0.0f, lp_tok = 0.0f, lse = 0.0f, H = 0.0f;
   if (mine) {
     lse = p.lse[at];
-    if (p.g_logp) {
+    if (p.tokens && p.logp) {
       tok = p.tokens[at];
-      gl = p.g_logp[at];
       lp_tok = p.logp[at];
     }
+    if (p.g_logp) gl = p.g_logp[at];
     if (p.g_entropy) {
       ge = p.g_entropy[at];
       H = p.entropy[at];
@@ -394,6 +394,20 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
   lse = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lse), one));
   H = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(H), one));
   const float GL = wave_add(gl), GE = wave_add(ge);
+  // What the rounding of lse left out: x - log p of a token is the same value in full,
+  // and its logit x is the one of type T nearest to lse + log p (the logits themselves may
+  // be overwritten already).  From the likeliest token, where its log p is short enough
+  // to be the better one; else 0.
+  const bool tells = tok >= 0 && 4.0f * fabsf(lp_tok) <= fabsf(lse);
+  float fix = 0.0f;
+  if (__ballot(tells)) {
+    T x_tok;
+    from_float(lse + lp_tok, x_tok);
+    fix = (lse - to_float(x_tok)) + lp_tok;
+    const int at_most = tells ? order_of(lp_tok) : INT_MIN, best = wave_max(at_most);
+    fix = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(fix), __builtin_ctzll(__ballot(at_most == best))));
+  }
+  const float by = exp_of(fix), GLf = GL * by, GEf = GE * by, Hf = H + fix;
   const bool nothing = !any || lse == -INFINITY;  // an empty row's outputs are constant
 
   for (int base = part * kChunk; base < p.V; base += p.parts * kChunk) {
@@ -428,12 +442,12 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
       }
       if (GE == 0.0f) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) x[j] = -exp_of(x[j] - lse) * GL;
+        for (int j = 0; j < kPer; ++j) x[j] = -exp_of(x[j] - lse) * GLf;
       } else {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
           const float lp = x[j] - lse;
-          x[j] = -exp_of(lp) * (GL + GE * (fmaxf(lp, kFar) + H));
+          x[j] = -exp_of(lp) * (GLf + GEf * (fmaxf(lp, kFar) + Hf));
         }
       }
       // the tokens' own columns, from their log probabilities: 1 - p is lost in x - lse where p is near 1
