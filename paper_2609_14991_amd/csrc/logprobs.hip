@@ -357,6 +357,7 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
   const int64_t job = (int64_t)blockIdx.x * 4 + wave;
   if (job >= (int64_t)p.M * p.parts) return;
   const int r = (int)(job / p.parts), part = (int)(job % p.parts);
+  int parts = p.parts;
   const T *row = static_cast<const T *>(p.logits) + r * p.stride;
   T *out = static_cast<T *>(p.grad) + r * p.g_stride;
 
@@ -406,11 +407,27 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
     fix = (lse - to_float(x_tok)) + lp_tok;
     const int at_most = tells ? order_of(lp_tok) : INT_MIN, best = wave_max(at_most);
     fix = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(fix), __builtin_ctzll(__ballot(at_most == best))));
+  } else if ((GL != 0.0f || GE != 0.0f) && fabsf(lse) >= 4096.0f && fabsf(lse) < INFINITY) {
+    // no token tells, and p would be off by 2^-12 or more: m and log s once more.  One
+    // wave takes the row, which in place no other may overwrite meanwhile.
+    if (part != 0) return;
+    parts = 1;
+    WaveStat ws = wave_stat_none();
+    for (int base = 0; base < p.V; base += kChunk) {
+      float x[kPer];
+      load_chunk(row, p.V, base, lane, x);
+      float top = fmaxf(x[0], -INFINITY);
+#pragma unroll
+      for (int j = 1; j < kPer; ++j) top = fmaxf(top, x[j]);
+      wave_stat_take(ws, x, top, wave_max(top));
+    }
+    const RowScore q = row_score(wave_stat_done(ws));
+    fix = (lse - q.m) - q.log_s;
   }
   const float by = exp_of(fix), GLf = GL * by, GEf = GE * by, Hf = H + fix;
   const bool nothing = !any || lse == -INFINITY;  // an empty row's outputs are constant
 
-  for (int base = part * kChunk; base < p.V; base += p.parts * kChunk) {
+  for (int base = part * kChunk; base < p.V; base += parts * kChunk) {
     const bool whole = base + kChunk <= p.V;
     float x[kPer];
     if (nothing) {

@@ -113,3 +113,41 @@ def test_gradient_of_large_logits_of_16_bits(dtype):
     tok[0, 1::2] = rng.integers(0, V, 4)
     gl, ge = (rng.standard_normal((1, 8)).astype(np.float32) for _ in range(2))
     _check(x, tok, None, 8, 1, gl, ge)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("V", [1, 5, 1024, 5000])
+def test_entropy_gradient_without_tokens(V, dtype):
+    """Where no token tells what the rounding of lse left out: rows of large logits and rows masked as a whole, whose
+    entropy's gradient is 0 (p is uniform), in place and not; and rows whose only slot chose no token."""
+    rng = np.random.default_rng(V)
+    values = [LOWEST[dtype], -30000.0, 60000.0, 0.0] + ([-1e9, 2.5e7] if dtype != "float16" else [])
+    n = len(values) + 2
+    x = torch.tensor(values + [9000.0, -9000.0])[None, :, None].expand(1, n, V).clone()
+    x[0, -2:] += torch.tensor(np.rint(rng.standard_normal((2, V)) * 2).astype(np.float32)) * 8
+    x = x.to(DTYPES[dtype])
+    xs = x.double().numpy()
+    ge = rng.standard_normal((1, n)).astype(np.float32)
+    none = np.full((1, n), -1)
+    for tok in (None, none):
+        _, (view, stride, tok_d, _, out) = _score(x, tok, None, n, 1, 0)
+        want, _ = O.gradient(xs, None, None, n, 1, None, ge)
+        ref = O.scores(xs, None, None, n, 1, 0)
+        tol = np.zeros_like(want)
+        for r in range(n):
+            q = O.row_stats(xs[0, r])
+            lp = np.abs(xs[0, r] - q["m"] - q["ls"])
+            # log s read twice, its error and the difference's; below 4096 lse's own rounding
+            e = ref["tol_lse"][0, r] - 2 * O.U32 * abs(q["lse"]) + O.U32 * (4 * lp + 4 * q["ls"] + 20)
+            e = e + (O.U32 * abs(q["lse"]) if abs(q["lse"]) < 4096 else 0.0)
+            tol[0, r] = abs(ge[0, r]) * q["p"] * ((lp + q["H"] + 1) * e + ref["tol_entropy"][0, r] + e) + 2.0 ** -126 * 200
+        tol = tol + O.half_step(np.abs(want) + tol, dtype)
+        args = (view, stride, 1, n, 1, V, tok_d, None, out["logp"] if tok is not None else None, out["entropy"], out["lse"], None,
+                torch.tensor(ge, device=dev()))
+        grad = torch.full((1, n, V), 7.0, dtype=x.dtype, device=dev())
+        F.token_logprobs_backward(*args, grad, V)
+        _near(grad.cpu().double().numpy(), want, tol, "apart")
+        over = view.clone()
+        F.token_logprobs_backward(over, V, *args[2:], over, V)
+        assert torch.equal(over, grad)
