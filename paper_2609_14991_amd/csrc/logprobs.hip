@@ -372,22 +372,21 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
   }
   int tok = -1;
   float gl = 0.0f, ge = 0.0f, lp_tok = 0.0f, lse = 0.0f, H = 0.0f;
+  const bool told = p.tokens && p.logp;
+  if (lane < slots && told) tok = p.tokens[at];  // of dead slots too: one out of range is told of
   if (mine) {
     lse = p.lse[at];
-    if (p.tokens && p.logp) {
-      tok = p.tokens[at];
-      lp_tok = p.logp[at];
-    }
+    if (told) lp_tok = p.logp[at];
     if (p.g_logp) gl = p.g_logp[at];
     if (p.g_entropy) {
       ge = p.g_entropy[at];
       H = p.entropy[at];
     }
-    if (tok < 0 || tok >= p.V) {
-      bad |= tok != -1;
-      tok = -1;
-      gl = 0.0f;
-    }
+  }
+  bad |= tok < -1 || tok >= p.V;
+  if (!mine || tok < 0 || tok >= p.V) {
+    tok = -1;
+    gl = 0.0f;
   }
   const unsigned long long any = __ballot(mine);
   if (__ballot(bad) && lane == 0) atomicOr(&g_score_status, FUSION_STATUS_BAD_TOKEN);

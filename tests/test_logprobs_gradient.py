@@ -151,3 +151,23 @@ def test_entropy_gradient_without_tokens(V, dtype):
         over = view.clone()
         F.token_logprobs_backward(over, V, *args[2:], over, V)
         assert torch.equal(over, grad)
+
+
+@pytest.mark.gpu
+def test_a_bad_token_of_a_dead_slot_is_told_of():
+    """As by the scores themselves; the gradient is that of the live slots."""
+    rng = np.random.default_rng(4)
+    x = torch.tensor(rng.standard_normal((1, 4, 60)).astype(np.float32))
+    tok, par = np.array([[3, 60, 5, -1]]), np.array([[0, -1, 2, -1]])
+    F.fusion_device_status()
+    _, (view, stride, tok_d, par_d, out) = _score(x, tok, par, 1, 4, 0)
+    assert F.fusion_device_status() == F.FUSION_STATUS_BAD_TOKEN
+    grad, one = torch.empty((1, 4, 60), device=dev()), torch.ones((1, 4), device=dev())
+    args = (view, stride, 1, 1, 4, 60, tok_d, par_d, out["logp"], out["entropy"], out["lse"])
+    for gl, ge in ((one, None), (one, one), (None, one)):
+        F.token_logprobs_backward(*args, gl, ge, grad, 60)
+        assert F.fusion_device_status() == F.FUSION_STATUS_BAD_TOKEN
+        assert (grad[0, [1, 3]] == 0).all() and torch.isfinite(grad).all() and (grad[0, [0, 2]] != 0).any()
+    # without tokens to look at there is nothing to tell of
+    F.token_logprobs_backward(view, stride, 1, 1, 4, 60, None, par_d, None, out["entropy"], out["lse"], None, one, grad, 60)
+    assert F.fusion_device_status() == 0
