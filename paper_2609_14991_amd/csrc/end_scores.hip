@@ -79,20 +79,21 @@ __device__ int32_t g_end_status;
 }  // namespace
 
 // the status bits of the end-of-stream kernel and of the scoring kernels, cleared
-// (fusion_device_status merges them with the fusion kernels' own)
+// (fusion_device_status merges them with the fusion kernels' own).  Both words are read
+// before either is cleared, so that an error on the way loses nothing, and one that holds
+// nothing is not written: a call without bits copies twice.
 int end_status_take(int32_t *bits) {
-  int32_t v = 0, zero = 0;
-  hipError_t e = hipMemcpyFromSymbol(&v, HIP_SYMBOL(g_end_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
-  if (e != hipSuccess) return hip_error(e, "hipMemcpyFromSymbol");
-  e = hipMemcpyToSymbol(HIP_SYMBOL(g_end_status), &zero, sizeof(int32_t), 0, hipMemcpyHostToDevice);
-  if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
-  for (auto take : {score_status_take, joint_score_status_take}) {
-    int32_t more = 0;
-    const int rc = take(&more);
-    if (rc != FUSION_OK) return rc;
-    v |= more;
-  }
-  *bits = v;
+  int32_t end = 0, score = 0, *word = nullptr;
+  const int32_t zero = 0;
+  const int rc = score_status_word(&word);
+  if (rc != FUSION_OK) return rc;
+  hipError_t e = hipMemcpyFromSymbol(&end, HIP_SYMBOL(g_end_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
+  if (e == hipSuccess) e = hipMemcpy(&score, word, sizeof(int32_t), hipMemcpyDeviceToHost);
+  if (e != hipSuccess) return hip_error(e, "reading the status words");
+  if (end) e = hipMemcpyToSymbol(HIP_SYMBOL(g_end_status), &zero, sizeof(int32_t), 0, hipMemcpyHostToDevice);
+  if (e == hipSuccess && score) e = hipMemcpy(word, &zero, sizeof(int32_t), hipMemcpyHostToDevice);
+  if (e != hipSuccess) return hip_error(e, "clearing the status words");
+  *bits = end | score;
   return FUSION_OK;
 }
 

@@ -19,8 +19,6 @@
 namespace fusion {
 namespace {
 
-__device__ int32_t g_joint_score_status;
-
 // Statistics of a row's 16 TN logits in four lanes (l, l ^ 16, l ^ 32, l ^ 48), in
 // all of them.  Four operations a logit, the exponential among them: (x - m) log2 e is
 // one fma of x, off by what the rounding of m log2 e left, the same for the whole row,
@@ -143,6 +141,7 @@ struct JoinArgs {
   const float *bias, *part;
   const int32_t *tokens, *parents;
   float *logp, *entropy, *lse;
+  int32_t *status;  // scoring's word: bit set when a token or parent is out of range
   int32_t M, N, K, B, n_col_tiles;
 };
 
@@ -225,7 +224,7 @@ __global__ void __launch_bounds__(256) joint_join_kernel(JoinArgs p) {
   if (p.logp) p.logp[m] = bad ? nan : !scored ? 0.0f : row_logp(q, x);
   if (p.entropy) p.entropy[m] = r == -2 ? nan : q.entropy;
   if (p.lse) p.lse[m] = r == -2 ? nan : q.lse;
-  if (bad) atomicOr(&g_joint_score_status, FUSION_STATUS_BAD_TOKEN);
+  if (bad) atomicOr(p.status, FUSION_STATUS_BAD_TOKEN);
 }
 
 constexpr TileShape<2, 4, 8, 4, 2> t256{};
@@ -265,16 +264,6 @@ int check_sizes(int64_t M, int32_t N, int32_t K) {
 
 }  // namespace
 
-int joint_score_status_take(int32_t *bits) {
-  int32_t v = 0, zero = 0;
-  hipError_t e = hipMemcpyFromSymbol(&v, HIP_SYMBOL(g_joint_score_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
-  if (e != hipSuccess) return hip_error(e, "hipMemcpyFromSymbol");
-  e = hipMemcpyToSymbol(HIP_SYMBOL(g_joint_score_status), &zero, sizeof(int32_t), 0, hipMemcpyHostToDevice);
-  if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
-  *bits = v;
-  return FUSION_OK;
-}
-
 }  // namespace fusion
 
 using namespace fusion;
@@ -305,6 +294,9 @@ extern "C" int joint_logprobs(const uint16_t *A, const uint16_t *W, const float 
   if (!logp && !entropy && !lse) return set_error(FUSION_E_ARG, "no output buffer");
   if (workspace_floats < workspace((int)M, V)) return set_error(FUSION_E_ARG, "workspace too small");
   if (!logp) tokens = nullptr;
+  int32_t *status = nullptr;
+  const int no_word = score_status_word(&status);
+  if (no_word != FUSION_OK) return no_word;
   const int nct = with_shape((int)M, V, [&](auto c) -> int {
     using C = decltype(c);
     const int cols = (V + C::BN - 1) / C::BN, rows = ((int)M + C::BM - 1) / C::BM;
@@ -317,7 +309,7 @@ extern "C" int joint_logprobs(const uint16_t *A, const uint16_t *W, const float 
   if (nct < 0) return set_error(FUSION_E_UNSUPPORTED, "too many tiles: split the call along T");
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return hip_error(e, "joint statistics launch");
-  const JoinArgs p{A, W, bias, workspace_, tokens, parents, logp, entropy, lse, (int32_t)M, V, K, B, nct};
+  const JoinArgs p{A, W, bias, workspace_, tokens, parents, logp, entropy, lse, status, (int32_t)M, V, K, B, nct};
   if (M >= 64 * kCus) hipLaunchKernelGGL(joint_join_kernel<1>, dim3((unsigned)((M + 63) / 64)), dim3(256), 0, stream, p);
   else hipLaunchKernelGGL(joint_join_kernel<4>, dim3((unsigned)((M + 15) / 16)), dim3(256), 0, stream, p);
   e = hipGetLastError();

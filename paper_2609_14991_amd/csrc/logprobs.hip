@@ -501,14 +501,11 @@ __global__ void __launch_bounds__(256) grad_kernel(GradArgs p) {
 
 }  // namespace
 
-// the status bits of the kernels above, cleared
-int score_status_take(int32_t *bits) {
-  int32_t v = 0, zero = 0;
-  hipError_t e = hipMemcpyFromSymbol(&v, HIP_SYMBOL(g_score_status), sizeof(int32_t), 0, hipMemcpyDeviceToHost);
-  if (e != hipSuccess) return hip_error(e, "hipMemcpyFromSymbol");
-  e = hipMemcpyToSymbol(HIP_SYMBOL(g_score_status), &zero, sizeof(int32_t), 0, hipMemcpyHostToDevice);
-  if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
-  *bits = v;
+int score_status_word(int32_t **word) {
+  void *p = nullptr;
+  const hipError_t e = hipGetSymbolAddress(&p, HIP_SYMBOL(g_score_status));
+  if (e != hipSuccess) return hip_error(e, "hipGetSymbolAddress");
+  *word = static_cast<int32_t *>(p);
   return FUSION_OK;
 }
 

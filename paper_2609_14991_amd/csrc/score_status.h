@@ -1,10 +1,9 @@
-// Status bits of the scoring kernels (logprobs.hip, joint_logprobs.hip), taken and
-// cleared; end_status_take hands them on to fusion_device_status with its own.
+// The status word of the scoring kernels (logprobs.hip, joint_logprobs.hip) on the
+// current device; end_status_take reads it with its own for fusion_device_status.
 #pragma once
 
 #include <cstdint>
 
 namespace fusion {
-int score_status_take(int32_t *bits);
-int joint_score_status_take(int32_t *bits);
+int score_status_word(int32_t **word);
 }  // namespace fusion
