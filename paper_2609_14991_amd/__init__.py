@@ -526,7 +526,8 @@ def _rows(logits, what="logits"):
 def score(logits, tokens=None, parents=None, B=1, k=0, stream=None):
     """Log probabilities [T, S * B] of the tokens that a decode (``run``) chose from logits [T, S * B, V],
     the entropies and log sum exps of the rows they were chosen on, and the k best alternatives
-    ``top`` and ``top_logp`` [T, S * B, k].  Without tokens the rows alone."""
+    ``top`` and ``top_logp`` [T, S * B, k].  Without tokens the rows alone.  Nothing is recorded for
+    autograd, whether logits require a gradient or not: ``score_backward`` gives it."""
     import torch
 
     T, H, V, stride = _rows(logits)
@@ -547,7 +548,8 @@ def score(logits, tokens=None, parents=None, B=1, k=0, stream=None):
 def score_backward(logits, scored, tokens=None, parents=None, B=1, grad_logp=None, grad_entropy=None, in_place=False,
                    stream=None):
     """The gradient with respect to logits of what ``score`` gave (``scored``) for the same arguments, of the
-    logits' type; ``in_place`` writes it over them."""
+    logits' type; ``in_place`` writes it over them (an autograd graph that saved them then refuses its backward
+    pass, as after any operation in place)."""
     import torch
 
     T, H, V, stride = _rows(logits)
@@ -564,6 +566,8 @@ def score_backward(logits, scored, tokens=None, parents=None, B=1, grad_logp=Non
         grad = logits if in_place else torch.empty((T, H, V), dtype=logits.dtype, device=logits.device)
     token_logprobs_backward(logits, stride, T, H // B, B, V, tokens, parents, scored["logp"], scored["entropy"], scored["lse"],
                             grad_logp, grad_entropy, grad, stride if in_place else V, stream)
+    if in_place and not logits.is_inference():
+        torch.autograd.graph.increment_version(logits)
     return grad
 
 
