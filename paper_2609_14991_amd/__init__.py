@@ -503,18 +503,25 @@ def project(A, W, bias=None, stream=None):
     return out
 
 
+def _here(t) -> bool:
+    """Whether a tensor is on the current device, where a call's kernels run."""
+    import torch
+
+    return t.is_cuda and t.get_device() == torch.cuda.current_device()
+
+
 def _want(t, what, dtype, shape):
-    """A device tensor of this type and shape (None in a shape: any size), its elements in order."""
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or len(t.shape) != len(shape) or any(
+    """A tensor on the current device of this type and shape (None in a shape: any size), its elements in order."""
+    if not _here(t) or t.dtype != dtype or not t.is_contiguous() or len(t.shape) != len(shape) or any(
             n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{what}: a contiguous CUDA tensor of {dtype}, shape {list(shape)}, is wanted")
+        raise ValueError(f"{what}: a contiguous tensor of {dtype} on the current CUDA device, shape {list(shape)}, is wanted")
     return t
 
 
 def _rows(logits, what="logits"):
     """T, H, V and the distance of the rows of logits [T, H, V], which may lie apart."""
-    if not logits.is_cuda or logits.dim() != 3 or _dtype(logits) < 0:
-        raise ValueError(f"{what}: a CUDA tensor [T, S * B, V] of float32, bfloat16 or float16 is wanted")
+    if not _here(logits) or logits.dim() != 3 or _dtype(logits) < 0:
+        raise ValueError(f"{what}: a tensor [T, S * B, V] of float32, bfloat16 or float16 on the current CUDA device is wanted")
     T, H, V = logits.shape
     # (a dimension of one row says nothing about their distance)
     stride = logits.stride(1) if H > 1 else logits.stride(0) if T > 1 else V
