@@ -530,6 +530,13 @@ def _rows(logits, what="logits"):
     return T, H, V, stride
 
 
+def _slots(H, B):
+    """S of S * B slots a frame."""
+    if B < 1 or H % B != 0:
+        raise ValueError("S * B rows a frame are wanted")
+    return H // B
+
+
 def score(logits, tokens=None, parents=None, B=1, k=0, stream=None):
     """Log probabilities [T, S * B] of the tokens that a decode (``run``) chose from logits [T, S * B, V],
     the entropies and log sum exps of the rows they were chosen on, and the k best alternatives
@@ -538,8 +545,7 @@ def score(logits, tokens=None, parents=None, B=1, k=0, stream=None):
     import torch
 
     T, H, V, stride = _rows(logits)
-    if H % B != 0:
-        raise ValueError("S * B rows a frame are wanted")
+    S = _slots(H, B)
     for t, what in ((tokens, "tokens"), (parents, "parents")):
         if t is not None:
             _want(t, what, torch.int32, (T, H))
@@ -547,7 +553,7 @@ def score(logits, tokens=None, parents=None, B=1, k=0, stream=None):
     with _made_for(stream):
         out = dict(logp=None if tokens is None else new(torch.float32), entropy=new(torch.float32), lse=new(torch.float32),
                    top=new(torch.int32, k) if k else None, top_logp=new(torch.float32, k) if k else None)
-    token_logprobs(logits, stride, T, H // B, B, V, tokens, parents, k, out["logp"], out["entropy"], out["lse"], out["top"],
+    token_logprobs(logits, stride, T, S, B, V, tokens, parents, k, out["logp"], out["entropy"], out["lse"], out["top"],
                    out["top_logp"], stream)
     return out
 
@@ -560,8 +566,7 @@ def score_backward(logits, scored, tokens=None, parents=None, B=1, grad_logp=Non
     import torch
 
     T, H, V, stride = _rows(logits)
-    if H % B != 0:
-        raise ValueError("S * B rows a frame are wanted")
+    S = _slots(H, B)
     for t, what, dt in ((tokens, "tokens", torch.int32), (parents, "parents", torch.int32), (grad_logp, "grad_logp", torch.float32),
                         (grad_entropy, "grad_entropy", torch.float32)):
         if t is not None:
@@ -571,7 +576,7 @@ def score_backward(logits, scored, tokens=None, parents=None, B=1, grad_logp=Non
             _want(scored[n], n, torch.float32, (T, H))
     with _made_for(stream):
         grad = logits if in_place else torch.empty((T, H, V), dtype=logits.dtype, device=logits.device)
-    token_logprobs_backward(logits, stride, T, H // B, B, V, tokens, parents, scored["logp"], scored["entropy"], scored["lse"],
+    token_logprobs_backward(logits, stride, T, S, B, V, tokens, parents, scored["logp"], scored["entropy"], scored["lse"],
                             grad_logp, grad_entropy, grad, stride if in_place else V, stream)
     if in_place and not logits.is_inference():
         torch.autograd.graph.increment_version(logits)
@@ -589,8 +594,7 @@ def score_projected(A, W, bias=None, tokens=None, parents=None, B=1, stream=None
     _want(W, "W", torch.bfloat16, (None, K))
     if bias is not None:
         _want(bias, "bias", torch.float32, (V,))
-    if H % B != 0:
-        raise ValueError("S * B rows a frame are wanted")
+    S = _slots(H, B)
     for t, what in ((tokens, "tokens"), (parents, "parents")):
         if t is not None:
             _want(t, what, torch.int32, (T, H))
@@ -598,7 +602,7 @@ def score_projected(A, W, bias=None, tokens=None, parents=None, B=1, stream=None
     with _made_for(stream):
         out = dict(logp=None if tokens is None else new(), entropy=new(), lse=new())
         work = torch.empty(joint_logprobs_workspace(T * H, V, K), dtype=torch.float32, device=A.device)
-    joint_logprobs(A, W, bias, K, T, H // B, B, V, tokens, parents, out["logp"], out["entropy"], out["lse"], work, stream)
+    joint_logprobs(A, W, bias, K, T, S, B, V, tokens, parents, out["logp"], out["entropy"], out["lse"], work, stream)
     return out
 
 

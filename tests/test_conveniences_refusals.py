@@ -72,3 +72,13 @@ def test_tensors_of_another_device_than_the_current_one(on):
     for _, call in _calls(on, 1):
         with pytest.raises(ValueError, match="current CUDA device"):
             call()
+
+
+@pytest.mark.parametrize("B", [0, -1, 3, 5])
+def test_slots_that_the_rows_are_no_multiple_of(on, B):
+    x, f, i = (on(t, 0) for t in (torch.zeros((2, 4, 8)), torch.zeros((2, 4)), torch.zeros((2, 4), dtype=torch.int32)))
+    A, W = on(torch.zeros((2, 4, 64)).bfloat16(), 0), on(torch.zeros((8, 64)).bfloat16(), 0)
+    for call in (lambda: F.score(x, i, None, B), lambda: F.score_projected(A, W, None, i, None, B),
+                 lambda: F.score_backward(x, dict(logp=f, entropy=f, lse=f), i, None, B, f)):
+        with pytest.raises(ValueError):
+            call()
