@@ -433,10 +433,11 @@ def joint_logprobs_workspace(M, V, K) -> int:
 
 
 def joint_logprobs(A, W, bias, K, T, S, B, V, tokens, parents, logp, entropy, lse, workspace, stream=None):
-    """Same arguments as the C call (the workspace's size is its tensor's); A and W bfloat16 (or int16 bit patterns)."""
+    """Same arguments as the C call (the workspace's size is its tensor's, float32 or any other type in order); A and W
+    bfloat16 (or int16 bit patterns)."""
     _check(lib().joint_logprobs(_at(A), _at(W), _at(bias), int(K), int(T), int(S), int(B), int(V), _at(tokens),
                                 _at(parents), _at(logp), _at(entropy), _at(lse), _at(workspace),
-                                workspace.numel(), _on(stream)))
+                                workspace.numel() * workspace.element_size() // 4, _on(stream)))
 
 
 def mx_scale_stride(K) -> int:

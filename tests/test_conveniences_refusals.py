@@ -82,3 +82,19 @@ def test_slots_that_the_rows_are_no_multiple_of(on, B):
                  lambda: F.score_backward(x, dict(logp=f, entropy=f, lse=f), i, None, B, f)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [torch.uint8, torch.bfloat16, torch.float32, torch.float64])
+def test_a_workspace_counts_by_its_bytes(dtype):
+    """joint_logprobs takes the workspace's size from its tensor: one of another type holds as many floats as its
+    bytes.  (Refused for its size before anything is launched.)"""
+    need = 4 * F.joint_logprobs_workspace(8, 50, 64)
+    size = torch.empty(0, dtype=dtype).element_size()
+    with pytest.raises(F.FusionError, match="workspace too small"):
+        F.joint_logprobs(Address(), Address(), None, 64, 1, 8, 1, 50, None, None, None, Address(), None,
+                         torch.zeros((need - 1) // size, dtype=dtype), stream=0)
+
+
+class Address:
+    def data_ptr(self):
+        return 4096
