@@ -396,11 +396,14 @@ def _on(stream):
     return _current[0](_current[1]())
 
 
+_unchanged = contextlib.nullcontext()
+
+
 def _made_for(stream):
     """Tensors made inside are made on ``stream`` (an address; None: the current stream): their memory goes from one
     use on that stream to the next one there, and not to the current stream's work while ``stream`` still uses it."""
     if stream is None:
-        return contextlib.nullcontext()
+        return _unchanged
     import torch
 
     return torch.cuda.stream(torch.cuda.ExternalStream(int(stream)))
@@ -471,9 +474,8 @@ def fusion_device_status(stream=None) -> int:
 # ---------------------------------------------------------------------------
 # conveniences that allocate the outputs with torch (still no compute here)
 #
-# ``stream`` is the address of the stream to work on.  What score, score_backward, score_projected, quantize,
-# dequantize and project_mx return was made on it, as a tensor of ``with torch.cuda.stream(...)``: another
-# stream that uses it waits for this one and calls record_stream.
+# ``stream`` is the address of the stream to work on.  What they return was made on it, as a tensor of
+# ``with torch.cuda.stream(...)``: another stream that uses it waits for this one and calls record_stream.
 # ---------------------------------------------------------------------------
 def step(lm, trie, logits, lm_state, boost_state, lam, beta, blank_id, k, blank_mode,
          want_fused=False, stream=None):
@@ -481,13 +483,14 @@ def step(lm, trie, logits, lm_state, boost_state, lam, beta, blank_id, k, blank_
 
     H, V = logits.shape
     dev = logits.device
-    out = dict(
-        tokens=torch.empty((H, k), dtype=torch.int32, device=dev),
-        scores=torch.empty((H, k), dtype=torch.float32, device=dev),
-        next_lm=torch.empty((H, k), dtype=torch.int32, device=dev),
-        next_boost=torch.empty((H, k), dtype=torch.int32, device=dev),
-        fused=torch.empty((H, V), dtype=torch.float32, device=dev) if want_fused else None,
-    )
+    with _made_for(stream):
+        out = dict(
+            tokens=torch.empty((H, k), dtype=torch.int32, device=dev),
+            scores=torch.empty((H, k), dtype=torch.float32, device=dev),
+            next_lm=torch.empty((H, k), dtype=torch.int32, device=dev),
+            next_boost=torch.empty((H, k), dtype=torch.int32, device=dev),
+            fused=torch.empty((H, V), dtype=torch.float32, device=dev) if want_fused else None,
+        )
     fusion_step(lm, trie, logits, lm_state, boost_state, H, V, lam, beta, blank_id, k, blank_mode,
                 out["fused"], out["tokens"], out["scores"], out["next_lm"], out["next_boost"], stream)
     return out
@@ -499,7 +502,8 @@ def project(A, W, bias=None, stream=None):
 
     M, K = A.shape
     N = W.shape[0]
-    out = torch.empty((M, N), dtype=torch.float32, device=A.device)
+    with _made_for(stream):
+        out = torch.empty((M, N), dtype=torch.float32, device=A.device)
     joint_project(A, W, bias, M, N, K, out, stream)
     return out
 
@@ -661,9 +665,10 @@ def run(lm, trie, logits, S, B, k, lam, beta, blank_id, blank_mode, lm_state, bo
 
     T, H, V = logits.shape
     dev = logits.device
-    tokens = torch.empty((T, H), dtype=torch.int32, device=dev)
-    parents = torch.empty((T, H), dtype=torch.int32, device=dev) if B > 1 else None
-    fused = torch.zeros((T, H, V), dtype=torch.float32, device=dev) if want_fused else None
+    with _made_for(stream):
+        tokens = torch.empty((T, H), dtype=torch.int32, device=dev)
+        parents = torch.empty((T, H), dtype=torch.int32, device=dev) if B > 1 else None
+        fused = torch.zeros((T, H, V), dtype=torch.float32, device=dev) if want_fused else None
     fusion_run(lm, trie, logits, T, S, B, V, k, lam, beta, blank_id, blank_mode, lm_state,
                boost_state, hyp_score, tokens, parents, fused, traffic, stream)
     return dict(tokens=tokens, parents=parents, fused=fused)
@@ -677,13 +682,14 @@ def step_lms(lms, alphas, trie, logits, lm_state, boost_state, beta, blank_id, k
     H, V = logits.shape
     dev = logits.device
     n = len(lms)
-    out = dict(
-        tokens=torch.empty((H, k), dtype=torch.int32, device=dev),
-        scores=torch.empty((H, k), dtype=torch.float32, device=dev),
-        next_lm=torch.empty((n, H, k), dtype=torch.int32, device=dev),
-        next_boost=torch.empty((H, k), dtype=torch.int32, device=dev),
-        fused=torch.empty((H, V), dtype=torch.float32, device=dev) if want_fused else None,
-    )
+    with _made_for(stream):
+        out = dict(
+            tokens=torch.empty((H, k), dtype=torch.int32, device=dev),
+            scores=torch.empty((H, k), dtype=torch.float32, device=dev),
+            next_lm=torch.empty((n, H, k), dtype=torch.int32, device=dev),
+            next_boost=torch.empty((H, k), dtype=torch.int32, device=dev),
+            fused=torch.empty((H, V), dtype=torch.float32, device=dev) if want_fused else None,
+        )
     fusion_step_lms(lms, alphas, trie, logits, lm_state, boost_state, H, V, beta, blank_id, k,
                     blank_mode, out["fused"], out["tokens"], out["scores"], out["next_lm"],
                     out["next_boost"], stream)
@@ -699,9 +705,10 @@ def run_lms(lms, alphas, trie, logits, S, B, k, beta, blank_id, blank_mode, lm_s
 
     T, H, V = logits.shape
     dev = logits.device
-    tokens = torch.empty((T, H), dtype=torch.int32, device=dev)
-    parents = torch.empty((T, H), dtype=torch.int32, device=dev) if B > 1 else None
-    fused = torch.zeros((T, H, V), dtype=torch.float32, device=dev) if want_fused else None
+    with _made_for(stream):
+        tokens = torch.empty((T, H), dtype=torch.int32, device=dev)
+        parents = torch.empty((T, H), dtype=torch.int32, device=dev) if B > 1 else None
+        fused = torch.zeros((T, H, V), dtype=torch.float32, device=dev) if want_fused else None
     fusion_run_lms(lms, alphas, trie, logits, T, S, B, V, k, beta, blank_id, blank_mode, lm_state,
                    boost_state, hyp_score, tokens, parents, fused, traffic,
                    FUSION_RUN_RECOMBINE if recombine else 0, hist, stream)
