@@ -239,7 +239,8 @@ int64_t tiles(C, int M, int N) {
   return (int64_t)((M + C::BM - 1) / C::BM) * ((N + C::BN - 1) / C::BN);
 }
 
-// the largest tile that fills the chip, as in joint_project
+// The largest tile that fills the chip.  (Of joint_project's rules the plain ones; its
+// finer ones follow its stores, and are not measured here.)
 template <class F>
 auto with_shape(int M, int N, F f) {
   if (tiles(t256, M, N) >= 1000 && N > 128) return f(t256);

@@ -228,7 +228,7 @@ struct ScoreArgs {
 // thirds of the rows, 185 us token by token and 166 so); a row nothing was chosen on is not.
 // Bound by memory in fp32 (25600 rows of 1024: 19 us without alternatives, 5.4 TB/s)
 // and by the vector units where alternatives are asked for or values are 16 bits (busy
-// 74 % of the time on the beam above, 87 % on 16000 x 8190 in bf16).
+// 73 % of the time on the beam above, 85 % on 16000 x 8190 in bf16).
 // (32 values a lane instead of 16: half the waves fit, 173 -> 204 us for 76800 rows
 // of 4096 in bf16 with 4 alternatives.)
 // beam: there are parents.
