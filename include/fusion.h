@@ -394,9 +394,10 @@ int token_logprobs(const void *logits, int32_t dtype, int64_t stride, int32_t T,
  *                the same stride; otherwise the two must not overlap
  * Sums are fp32 in a fixed order, rounded once to dtype.  A token's own column comes
  * from logp, and so does what the rounding of lse left out of p = e^(x - lse): with
- * tokens and logp given, also where grad_logp is NULL, p is off by a few 2^-24 of log p of
- * itself, and at most by half a last place of lse.  Without a token on a row it is half a
- * last place of lse, but where that is past +-4096 the row is read twice instead.  The
+ * tokens and logp given, also where grad_logp is NULL, the relative error of p is a few
+ * 2^-24 times log p of the row's likeliest token, and at most half a last place of lse.
+ * Without a token on a row it is half a last place of lse, but where lse is past +-4096
+ * the row is read twice instead.  The
  * alternatives have no gradient.  A token out of range counts as none, a parent out of
  * range as a dead slot, and FUSION_STATUS_BAD_TOKEN is set.  Only enqueues work on
  * `stream`; no workspace.
